@@ -1,0 +1,365 @@
+"""The operators of a Transformer layer's feed-forward half, as cases that can be timed: their plain
+forms in elementary torch operations (`own` false) and this library's kernels (`own` true).
+
+A case is a dict of plain values:
+
+  op        "linear"      y = act(x w^T + bias) + residual, with the pre-activation kept for the backward
+            "linear_bwd"  dx = (dy w) act'(z) + residual's gradient, dw = dy^T x, dbias = sum of dy
+            "activation"  dz = dy act'(z)
+            "checkpoint"  x -> 8 bits -> x
+  B, N      sequences, tokens per sequence;  pad: the longest sequences' tail that is padding, as a share
+            of N (sequence b ends in an amount of padding that follows from b alone)
+  E, F      features in and out ("activation", "checkpoint": E alone)
+  act       activation of the epilogue, or, backward, the one whose pre-activation is z
+  bias, residual   whether there is one (backward: whether a gradient is added to dx)
+  z         what is kept of the pre-activation, or comes from it: "", "bf16" or "8bit"
+  x         backward: how x was kept, "bf16" or "8bit"
+  dtype     "checkpoint": of the values, "bf16" or "f32"
+
+Eight bits are e4m3 codes with one power-of-two scale for each 32 features of a token: the smallest
+that keeps the block's largest value within 448.  They are returned as the values that they stand for.
+"""
+import math
+
+import numpy as np
+import torch
+
+own = False
+
+BLOCK = 32
+ACTS = ("none", "relu", "gelu", "gelu_tanh", "silu", "tanh")
+
+
+def _case(name, op, B, N, E, F=0, pad=0.0, act="none", bias=False, residual=False, z="", x="bf16", dtype="bf16"):
+    c = dict(op=op, B=B, N=N, E=E, F=F, pad=pad, act=act, bias=bias, residual=residual, z=z, x=x, dtype=dtype)
+    return dict(c, name=name) if name else c
+
+
+def listed():
+    return [
+        # one token through a hidden layer, where latency counts: the head on a table's first token
+        _case("one token", "linear", 1, 1, 768, 768, act="gelu", bias=True),
+        # a few questions' tokens through the wide product of a large layer: its weights are what is read
+        _case("24 tokens, wide", "linear", 4, 6, 1024, 4096, act="gelu", bias=True),
+        # serving one table: the product back to the model's width, with the layer's input added
+        _case("serving 1999 tokens", "linear", 1, 1999, 4096, 1024, bias=True, residual=True),
+        # widths that no tile divides, a batch whose sequences end in padding, everything in the epilogue
+        _case("ragged, odd widths", "linear", 7, 333, 760, 1288, pad=0.5, act="silu", bias=True, residual=True, z="bf16"),
+        # the wide product of a large layer that trains on long tables, its pre-activation kept in 8 bits
+        _case("training at 8192, wide", "linear", 2, 8192, 1024, 4096, pad=0.1, act="gelu", bias=True, z="8bit"),
+        # fine-tuning a base-size layer with 16-bit activations: the product back to the model's width
+        _case("backward, fine-tuning at 509", "linear_bwd", 8, 509, 2048, 768, pad=0.4, act="gelu", bias=True, z="bf16"),
+        # the same product of a large layer on long tables, from 8-bit checkpoints of its input
+        _case("backward at 8192, narrow", "linear_bwd", 2, 8192, 4096, 1024, pad=0.1, act="gelu", bias=True, z="8bit", x="8bit"),
+        # and the wide one, whose input's gradient is joined by the one that went round the layer
+        _case("backward at 8192, wide", "linear_bwd", 2, 8192, 1024, 4096, pad=0.1, bias=True, residual=True, x="8bit"),
+        # a head's activation on its own, a batch of first tokens
+        _case("activation, 48 rows", "activation", 48, 1, 768, act="tanh", z="bf16"),
+        # the same for a product whose gradient could not be joined, from its 8-bit checkpoint
+        _case("activation at 8192", "activation", 2, 8192, 4096, pad=0.1, act="gelu", z="8bit"),
+        # what one short sequence keeps, in fp32
+        _case("checkpoint, 37 rows", "checkpoint", 1, 37, 768, dtype="f32"),
+        # what a large layer keeps of a long batch
+        _case("checkpoint at 8192", "checkpoint", 2, 8192, 4096, pad=0.1),
+    ]
+
+
+def _log_uniform(rng, lo, hi):
+    return min(hi, max(lo, int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))))
+
+
+_most = {}
+
+
+def _limit(op):
+    if not _most:
+        for c in listed():
+            w = work(c)
+            f, b = _most.get(c["op"], (0, 0))
+            _most[c["op"]] = (max(f, w["flops"]), max(b, w["bytes"]))
+    return _most[op]
+
+
+def draw(rng):
+    op = rng.choice(["linear", "linear", "linear_bwd", "linear_bwd", "activation", "checkpoint"])
+    B, N = _log_uniform(rng, 1, 32), _log_uniform(rng, 1, 8192)
+    E, F = (8 * _log_uniform(rng, 8, 512) for _ in range(2))
+    pad = rng.choice([0.0, 0.1, 0.5]) if N > 1 else 0.0
+    act = rng.choice(ACTS)
+    c = _case(None, op, B, N, E, pad=pad)
+    if op == "linear":
+        c.update(F=F, act=act, bias=rng.random() < 0.8, residual=rng.random() < 0.5, z=rng.choice(["", "bf16", "8bit"]))
+    elif op == "linear_bwd":
+        c.update(F=F, act=act, z="" if act == "none" else rng.choice(["bf16", "8bit"]), bias=rng.random() < 0.8,
+                 residual=rng.random() < 0.5, x=rng.choice(["bf16", "8bit"]))
+    elif op == "activation":
+        c.update(act=rng.choice(ACTS[1:]), z=rng.choice(["bf16", "8bit"]))
+    else:
+        c.update(dtype=rng.choice(["bf16", "f32"]))
+    flops, bytes_ = _limit(op)
+    while True:
+        w = work(c)
+        if w["flops"] <= flops and w["bytes"] <= bytes_:
+            return c
+        if c["B"] > 1:
+            c["B"] = c["B"] * 3 // 4
+        elif c["N"] > 64:
+            c["N"] = c["N"] * 3 // 4
+        else:
+            c["E"] = c["E"] * 3 // 32 * 8
+
+
+def _lengths(case):
+    """Tokens of each sequence that are not padding."""
+    return [case["N"] - int(case["N"] * case["pad"] * math.modf((b + 1) * 0.618034)[0]) for b in range(case["B"])]
+
+
+class _State:
+    pass
+
+
+def _kept(x):
+    """x in 8 bits, as codes and scales."""
+    rows, E = x.shape[:-1], x.shape[-1]
+    blocks = torch.nn.functional.pad(x.float(), (0, -E % BLOCK)).view(*rows, -1, BLOCK)
+    m, e = torch.frexp(blocks.abs().amax(-1))
+    code = (e - 9 + (m > 0.875) + 127).clamp(1, 254)   # the largest value is m 2^e, and 448 is 0.875 2^9
+    codes = torch.ldexp(blocks, (127 - code)[..., None]).to(torch.float8_e4m3fn).view(torch.uint8)
+    return codes.view(*rows, -1)[..., :E].contiguous(), code.to(torch.uint8)
+
+
+def prepare(case, seed):
+    s = _State()
+    s.case = case
+    B, N, E, F, op = case["B"], case["N"], case["E"], case["F"], case["op"]
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+
+    def normal(*shape, scale=1.0, dtype=torch.bfloat16):
+        return torch.randn(shape, device="cuda", generator=gen).mul_(scale).to(dtype)
+
+    # 0: a table's token, 1: a question's, 2: padding
+    at = torch.arange(N, device="cuda")
+    ends = torch.tensor(_lengths(case), device="cuda")[:, None]
+    s.flags = torch.where(at >= ends, 2, (at < N // 16).int()).to(torch.uint8).contiguous()
+    s.x = s.x8 = s.z = s.z8 = s.bias = s.residual = None
+    if op == "checkpoint":
+        # activations: most near one, some features of every token far larger
+        s.x = normal(B, N, E, dtype=torch.float32)
+        s.x *= torch.exp2(torch.randn(E, device="cuda", generator=gen) * 2)
+        s.x = s.x.to(torch.float32 if case["dtype"] == "f32" else torch.bfloat16)
+        return s
+    if op == "activation":
+        s.dy, s.z = normal(B, N, E, scale=0.02), normal(B, N, E, scale=1.5)
+    elif op == "linear":
+        s.x, s.w = normal(B, N, E), normal(F, E, scale=E ** -0.5)
+        s.bias = normal(F, scale=0.1, dtype=torch.float32) if case["bias"] else None
+        s.residual = normal(B, N, F) if case["residual"] else None
+        return s
+    else:
+        s.dy, s.w = normal(B, N, F, scale=0.02), normal(F, E, scale=E ** -0.5)
+        s.x, s.z = normal(B, N, E), normal(B, N, E) if case["z"] else None
+        s.residual = normal(B, N, E, scale=0.02) if case["residual"] else None
+        if case["x"] == "8bit":
+            s.x8, s.x = _kept(s.x), None
+    if case["z"] == "8bit":
+        s.z8, s.z = _kept(s.z), None
+    return s
+
+
+# ---- the plain forms, in 32 bits --------------------------------------------------------------------
+def _values(codes, scales):
+    """What codes and scales stand for."""
+    scale = torch.repeat_interleave(scales.int() - 127, BLOCK, dim=-1)[..., :codes.shape[-1]]
+    return torch.ldexp(codes.view(torch.float8_e4m3fn).float(), scale)
+
+
+def _act(name, z):
+    if name == "relu":
+        return torch.where(z > 0, z, 0)
+    if name == "gelu":
+        return 0.5 * z * (1 + torch.erf(z * math.sqrt(0.5)))
+    if name == "gelu_tanh":
+        return 0.5 * z * (1 + torch.tanh(math.sqrt(2 / math.pi) * (z + 0.044715 * z * z * z)))
+    if name == "silu":
+        return z / (1 + torch.exp(-z))
+    if name == "tanh":
+        return torch.tanh(z)
+    return z
+
+
+def _slope(name, z):
+    if name == "relu":
+        return (z > 0).to(z.dtype)
+    if name == "gelu":
+        return 0.5 * (1 + torch.erf(z * math.sqrt(0.5))) + z * torch.exp(-0.5 * z * z) * (0.5 / math.pi) ** 0.5
+    if name == "gelu_tanh":
+        t = torch.tanh(math.sqrt(2 / math.pi) * (z + 0.044715 * z * z * z))
+        return 0.5 * (1 + t) + 0.5 * z * (1 - t * t) * math.sqrt(2 / math.pi) * (1 + 3 * 0.044715 * z * z)
+    if name == "silu":
+        p = 1 / (1 + torch.exp(-z))
+        return p * (1 + z * (1 - p))
+    if name == "tanh":
+        t = torch.tanh(z)
+        return 1 - t * t
+    return torch.ones_like(z)
+
+
+def _plain(s):
+    case = s.case
+    op, act = case["op"], case["act"]
+    live = (s.flags < 2)[..., None]
+    if op == "checkpoint":
+        return {"x": torch.where(live, _values(*_kept(s.x)), 0).to(s.x.dtype)}
+    z = _values(*s.z8) if s.z8 else s.z.float() if s.z is not None else None
+    if op == "activation":
+        return {"dz": torch.where(live, s.dy.float() * _slope(act, z), 0).bfloat16()}
+    if op == "linear":
+        z = torch.matmul(s.x.float(), s.w.float().t())
+        if case["bias"]:
+            z = z + s.bias
+        y = _act(act, z)
+        if case["residual"]:
+            y = y + s.residual.float()
+        out = {"y": torch.where(live, y, 0).bfloat16()}
+        if case["z"]:
+            z = torch.where(live, z, 0)
+            out["z"] = (_values(*_kept(z)) if case["z"] == "8bit" else z).bfloat16()
+        return out
+    g = torch.where(live, s.dy.float(), 0)
+    x = torch.where(live, _values(*s.x8) if s.x8 else s.x.float(), 0)
+    dx = torch.matmul(g, s.w.float())
+    if z is not None:
+        dx = dx * _slope(act, z)
+    if case["residual"]:
+        dx = dx + s.residual.float()
+    out = {"dx": torch.where(live, dx, 0).bfloat16()}
+    g = g.flatten(0, 1)
+    out["dw"] = torch.matmul(g.t(), x.flatten(0, 1))
+    if case["bias"]:
+        out["dbias"] = g.sum(0)
+    return out
+
+
+# ---- the library's calls ----------------------------------------------------------------------------
+def _library(s):
+    from paper_2109_04312_amd import mate
+
+    case = s.case
+    op, act = case["op"], getattr(mate, "MATE_ACT_" + case["act"].upper())
+    if op == "checkpoint":
+        return {"x": mate.checkpoint_unpack(mate.checkpoint_pack(s.x, s.flags), s.x.dtype)}
+    z = mate.Checkpoint(*s.z8) if s.z8 else s.z
+    if op == "activation":
+        return {"dz": mate.activation_bwd(s.dy, z, act, s.flags)}
+    if op == "linear":
+        keep = {"": mate.MATE_KEEP_NONE, "bf16": mate.MATE_KEEP_BF16, "8bit": mate.MATE_KEEP_8BIT}[case["z"]]
+        y, z = mate.linear(s.x, s.w, s.bias, s.flags, act=act, residual=s.residual, keep_z=keep)
+        if not case["z"]:
+            return {"y": y}
+        return {"y": y, "z": mate.checkpoint_unpack(z, torch.bfloat16) if case["z"] == "8bit" else z}
+    x = mate.Checkpoint(*s.x8) if s.x8 else s.x
+    dx, dw, dbias = mate.linear_bwd(s.dy, x, s.w, s.flags, z=z, act=act, residual=s.residual, want_dbias=case["bias"])
+    out = {"dx": dx, "dw": dw}
+    if case["bias"]:
+        out["dbias"] = dbias
+    return out
+
+
+def run(s):
+    return _library(s) if own else _plain(s)
+
+
+# ---- 64 bits, from the definitions ------------------------------------------------------------------
+def _exact_kept(v):
+    """The nearest values that 8 bits can hold, ties to the even one, block by block."""
+    E = v.shape[-1]
+    blocks = torch.cat([v, v.new_zeros(*v.shape[:-1], -E % BLOCK)], -1).unflatten(-1, (-1, BLOCK))
+    most = blocks.abs().amax(-1, keepdim=True)
+    scale = torch.exp2(torch.ceil(torch.log2(most.clamp_min(2.0 ** -126 * 448) / 448)))
+    u = blocks / scale
+    step = torch.exp2(torch.floor(torch.log2(u.abs().clamp_min(2.0 ** -6))) - 3)
+    return (torch.round(u / step) * step * scale).flatten(-2)[..., :E]
+
+
+def _exact_values(codes, scales):
+    c = codes.to(torch.int64)
+    e, m = (c >> 3) & 15, (c & 7).double()
+    v = torch.where(e > 0, (1 + m / 8) * torch.exp2(e.double() - 7), m * 2.0 ** -9) * (1 - 2 * (c >> 7)).double()
+    block = torch.arange(codes.shape[-1], device=codes.device) // BLOCK
+    return v * torch.exp2(scales.double() - 127)[..., block]
+
+
+def _normal_cdf(z):
+    return 0.5 * torch.special.erfc(-z / math.sqrt(2.0))
+
+
+def _exact_act(name, z):
+    """(value, derivative)"""
+    if name == "relu":
+        return z.clamp_min(0.0), torch.heaviside(z, torch.zeros_like(z))
+    if name == "gelu":
+        return z * _normal_cdf(z), _normal_cdf(z) + z * torch.exp(-z.square() / 2) / math.sqrt(2 * math.pi)
+    if name == "gelu_tanh":
+        # 1 + tanh u = 2 sigmoid(2 u)
+        a = math.sqrt(8 / math.pi)
+        p = torch.sigmoid(a * (z + 0.044715 * z ** 3))
+        return z * p, p + z * p * (1 - p) * a * (1 + 0.134145 * z ** 2)
+    if name == "silu":
+        p = torch.sigmoid(z)
+        return z * p, p + z * p * torch.sigmoid(-z)
+    if name == "tanh":
+        return torch.tanh(z), torch.cosh(z.clamp(-300, 300)) ** -2
+    return z, torch.ones_like(z)
+
+
+def exact(case, seed):
+    s = prepare(case, seed)
+    op, act = case["op"], case["act"]
+    pad = (s.flags >= 2)[..., None]
+    if op == "checkpoint":
+        return {"x": _exact_kept(s.x.double()).masked_fill(pad, 0.0)}
+    z = _exact_values(*s.z8) if s.z8 else s.z.double() if s.z is not None else None
+    if op == "activation":
+        return {"dz": (s.dy.double() * _exact_act(act, z)[1]).masked_fill(pad, 0.0)}
+    if op == "linear":
+        z = s.x.double() @ s.w.double().T
+        if s.bias is not None:
+            z += s.bias.double()
+        y = _exact_act(act, z)[0]
+        if s.residual is not None:
+            y = y + s.residual.double()
+        out = {"y": y.masked_fill(pad, 0.0)}
+        if case["z"]:
+            out["z"] = (_exact_kept(z) if case["z"] == "8bit" else z).masked_fill(pad, 0.0)
+        return out
+    g = s.dy.double().masked_fill(pad, 0.0)
+    x = (_exact_values(*s.x8) if s.x8 else s.x.double()).masked_fill(pad, 0.0)
+    dx = g @ s.w.double()
+    if z is not None:
+        dx = dx * _exact_act(act, z)[1]
+    if s.residual is not None:
+        dx = dx + s.residual.double()
+    g, x = g.reshape(-1, case["F"]), x.reshape(-1, case["E"])
+    out = {"dx": dx.masked_fill(pad, 0.0), "dw": g.T @ x}
+    if case["bias"]:
+        out["dbias"] = torch.ones(len(g), dtype=torch.float64, device=g.device) @ g
+    return out
+
+
+def work(case):
+    B, N, E, F, op = case["B"], case["N"], case["E"], case["F"], case["op"]
+    T, live = B * N, int(np.sum(_lengths(case)))
+    kept = {"": 0.0, "bf16": 2.0 * E, "8bit": E + -(-E // BLOCK)}   # bytes a token
+    if op == "checkpoint":   # values -> codes and scales -> values
+        size = 4 if case["dtype"] == "f32" else 2
+        return {"bytes": float(T + size * E * (live + T) + 2 * T * kept["8bit"]), "flops": 0.0}
+    if op == "activation":   # dy and z -> dz
+        return {"bytes": float(T + 2 * E * (live + T) + live * kept[case["z"]]), "flops": 0.0}
+    if op == "linear":
+        bytes_ = T + 2 * live * E + 2 * E * F + (4 * F if case["bias"] else 0) + (2 * live * F if case["residual"] else 0) + 2 * T * F
+        if case["z"]:   # written; and, where it is 8 bits, read and written as values
+            bytes_ += 2 * T * F + (2 * T * (F + -(-F // BLOCK)) if case["z"] == "8bit" else 0)
+        return {"bytes": float(bytes_), "flops": 2.0 * live * E * F}
+    bytes_ = T + 2 * live * F + 2 * E * F + live * (kept[case["x"]] + kept[case["z"]]) + (2 * live * E if case["residual"] else 0)
+    bytes_ += 2 * T * E + 4 * E * F + (4 * F if case["bias"] else 0)
+    return {"bytes": float(bytes_), "flops": 4.0 * live * E * F}
