@@ -118,13 +118,18 @@ class _State:
     pass
 
 
+def _power(e):
+    """2^e, exact (torch.ldexp on a GPU is not, for some e); -126 <= e <= 127."""
+    return ((e + 127) << 23).view(torch.float32)
+
+
 def _kept(x):
     """x in 8 bits, as codes and scales."""
     rows, E = x.shape[:-1], x.shape[-1]
     blocks = torch.nn.functional.pad(x.float(), (0, -E % BLOCK)).view(*rows, -1, BLOCK)
     m, e = torch.frexp(blocks.abs().amax(-1))
     code = (e - 9 + (m > 0.875) + 127).clamp(1, 254)   # the largest value is m 2^e, and 448 is 0.875 2^9
-    codes = torch.ldexp(blocks, (127 - code)[..., None]).to(torch.float8_e4m3fn).view(torch.uint8)
+    codes = (blocks * _power(127 - code)[..., None]).to(torch.float8_e4m3fn).view(torch.uint8)
     return codes.view(*rows, -1)[..., :E].contiguous(), code.to(torch.uint8)
 
 
@@ -169,8 +174,8 @@ def prepare(case, seed):
 # ---- the plain forms, in 32 bits --------------------------------------------------------------------
 def _values(codes, scales):
     """What codes and scales stand for."""
-    scale = torch.repeat_interleave(scales.int() - 127, BLOCK, dim=-1)[..., :codes.shape[-1]]
-    return torch.ldexp(codes.view(torch.float8_e4m3fn).float(), scale)
+    scale = torch.repeat_interleave(_power(scales.int() - 127), BLOCK, dim=-1)[..., :codes.shape[-1]]
+    return codes.view(torch.float8_e4m3fn).float() * scale
 
 
 def _act(name, z):
