@@ -42,7 +42,8 @@ typedef enum {
   MATE_OK = 0,
   MATE_ERR_NULL = -1,        /* a required pointer is NULL                                */
   MATE_ERR_SHAPE = -2,       /* B, H, N out of range, or tables built for another (B, N)  */
-  MATE_ERR_UNSUPPORTED = -3, /* D != 64, unknown dtype or head kind, scale not positive   */
+  MATE_ERR_UNSUPPORTED = -3, /* D != 64, unknown dtype or head kind, scale not positive; a width,
+                                activation or address that the products with an epilogue refuse */
   MATE_ERR_WORKSPACE = -4,   /* workspace_bytes smaller than mate_workspace_bytes(...), or an
                                 address that the bf16 attention's 64-bit atomics cannot use
                                 (not a multiple of 8)                                      */
@@ -342,6 +343,78 @@ mate_status mate_out_project_bwd(const void* o, const void* w_o, const uint8_t* 
                                  const void* dy, int B, int N, int H, int E, mate_dtype t,
                                  void* d_o, float* dw_o, float* dbias, void* workspace,
                                  size_t workspace_bytes, void* stream);
+
+/*
+ * The feed-forward half of a Transformer layer: products with an epilogue, bf16 on the matrix cores, the
+ * gradients of both, and activations kept in 8 bits from the forward to the backward pass.  (The paper's layers
+ * have that half and train through it; its equations stop at the attention head.)
+ *
+ * Rows are the B * N tokens; `flags` as above, or NULL if no token is padding.  Widths (E, F) are multiples of 8, 8 to
+ * 65536; addresses multiples of 16 (flags and scales: any).  t: MATE_BF16 only, otherwise MATE_ERR_UNSUPPORTED.
+ *
+ * 8 bits.  A tensor of [B, N, W] values is `codes` [B, N, W] uint8, e4m3 (1 sign, 4 exponent, 3 mantissa bits, no
+ * infinities), and `scales` [B, N, ceil(W / 32)] uint8, one for each 32 features of a token (the last block may be
+ * shorter): value = code * 2^(scale - 127).  A scale is the smallest with the block's largest finite magnitude
+ * <= 448 * 2^(scale - 127), at least 1: no finite value saturates, each is off by 2^-4 of itself at most, or
+ * by 2^-10 of 2^(scale - 127) if that is more.  Rounded to nearest even (from 1.9375 * 2^127 on down,
+ * to 1.875 * 2^127).  Infinities and NaN are kept as NaN.  Rows of PAD tokens
+ * are kept as zeros.
+ *
+ * mate_linear:  z = x w^T + bias,   y = act(z) + residual
+ *   x         [B, N, E] bf16        w      [F, E] bf16        bias    [F] float, may be NULL
+ *   residual  [B, N, F] bf16, may be NULL; may be y itself
+ *   y         [B, N, F] bf16
+ *   z         NULL: not kept; z_scales NULL: [B, N, F] bf16; else codes, with z_scales
+ *   y_codes, y_scales   y in 8 bits as well, for the backward of the product that reads y; or both NULL
+ * z and y are rounded once, from fp32 (8 bits of either too: not from its bf16).  Rows of PAD tokens of every result are zeros.
+ *
+ * mate_linear_bwd:  with G = dy, its rows of PAD tokens counting as zero,
+ *     dx    = (G w) * act'(z) + residual    [B, N, E] bf16, rows of PAD tokens written 0
+ *     dw    = sum over non-pad tokens of G^T x    [F, E] float
+ *     dbias = sum over non-pad tokens of G        [F] float
+ *   x         x_scales NULL: [B, N, E] bf16; else codes.  May be NULL if dw is
+ *   w         may be NULL if dx is
+ *   z         the pre-activation that x came from, x = act(z): [B, N, E] bf16, or codes if z_scales is not NULL; NULL if x is
+ *             no activation (act is MATE_ACT_NONE then, and z NULL)
+ *   residual  gradient that reached x on another way, [B, N, E] bf16, or NULL; may be dx itself
+ *   dx, dw, dbias   any may be NULL (not computed); dbias needs dw
+ *   workspace mate_linear_bwd_workspace_bytes(B, N, E, F, x_scales != NULL) bytes (0: sizes out of range); needed for dw only
+ * A layer y = act(x w^T + b) whose next product is y w2^T: mate_linear_bwd of the second with z and act of the first gives the
+ * gradient at z, which is dy of the first one's mate_linear_bwd.  The result does not depend on whether the other gradient is wanted.
+ *
+ * mate_activation_bwd:  dz = dy * act'(z), rows of PAD tokens 0, for an activation that no product follows
+ *   dy, dz [B, N, E] bf16 (may be the same);  z as in mate_linear_bwd;  act not MATE_ACT_NONE
+ *
+ * mate_checkpoint_pack: x -> codes, scales;  mate_checkpoint_unpack: codes, scales -> x.  x: [B, N, E] of dtype t, MATE_BF16 or MATE_F32.
+ *
+ * fp32 accumulation throughout.  Asynchronous on `stream`; deterministic.
+ */
+typedef enum {
+  MATE_ACT_NONE = 0,
+  MATE_ACT_RELU = 1,
+  MATE_ACT_GELU = 2,      /* z times the normal distribution function at z       */
+  MATE_ACT_GELU_TANH = 3, /* 0.5 z (1 + tanh(sqrt(2 / pi) (z + 0.044715 z^3)))   */
+  MATE_ACT_SILU = 4,      /* z / (1 + exp(-z))                                   */
+  MATE_ACT_TANH = 5
+} mate_activation;
+enum { MATE_SCALE_BLOCK = 32 /* features that share a scale */, MATE_MAX_WIDTH = 65536 };
+mate_status mate_linear(const void* x, const void* w, const float* bias, const uint8_t* flags,
+                        const void* residual, int B, int N, int E, int F, mate_activation act,
+                        mate_dtype t, void* y, void* z, uint8_t* z_scales, uint8_t* y_codes,
+                        uint8_t* y_scales, void* stream);
+size_t mate_linear_bwd_workspace_bytes(int B, int N, int E, int F, int x_in_codes);
+mate_status mate_linear_bwd(const void* dy, const void* x, const uint8_t* x_scales, const void* w,
+                            const uint8_t* flags, const void* z, const uint8_t* z_scales,
+                            const void* residual, int B, int N, int E, int F, mate_activation act,
+                            mate_dtype t, void* dx, float* dw, float* dbias, void* workspace,
+                            size_t workspace_bytes, void* stream);
+mate_status mate_activation_bwd(const void* dy, const void* z, const uint8_t* z_scales,
+                                const uint8_t* flags, int B, int N, int E, mate_activation act,
+                                mate_dtype t, void* dz, void* stream);
+mate_status mate_checkpoint_pack(const void* x, const uint8_t* flags, int B, int N, int E,
+                                 mate_dtype t, uint8_t* codes, uint8_t* scales, void* stream);
+mate_status mate_checkpoint_unpack(const uint8_t* codes, const uint8_t* scales, int B, int N, int E,
+                                   mate_dtype t, void* x, void* stream);
 
 /*
  * Measurement hook, not part of the computation: arms the calling thread so that the next

@@ -6,9 +6,12 @@
 #include <algorithm>
 #include <atomic>
 #include <cstring>
+#include <initializer_list>
 #include <random>
 
 #include "../../include/mate.h"
+#include "activation.h"
+#include "eight_bits.h"
 #include "launch.h"
 #include "seg_layout.h"
 #include "stream_plan.h"
@@ -300,6 +303,78 @@ mate_status mate_out_project_bwd(const void* o, const void* w_o, const uint8_t* 
   return e == hipSuccess ? MATE_OK : MATE_ERR_HIP;
 }
 
+namespace {
+// Tokens are numbered in 32 bits, with room for the tile behind the last.
+bool tokens_ok(int B, int N) { return shape_ok(B, N) && (long long)B * N <= 0x7fffffffll - 1024; }
+bool width_ok(int W) { return W >= 8 && W <= MATE_MAX_WIDTH && W % 8 == 0; }
+bool aligned(std::initializer_list<const void*> ps) {
+  for (const void* p : ps)
+    if (reinterpret_cast<uintptr_t>(p) % 16) return false;
+  return true;
+}
+bool act_ok(mate_activation act) { return act >= MATE_ACT_NONE && act <= MATE_ACT_TANH; }
+static_assert(MATE_ACT_NONE == kActNone && MATE_ACT_RELU == kActRelu && MATE_ACT_GELU == kActGelu && MATE_ACT_GELU_TANH == kActGeluTanh &&
+                  MATE_ACT_SILU == kActSilu && MATE_ACT_TANH == kActTanh && MATE_SCALE_BLOCK == kScaleBlock,
+              "header and kernels disagree");
+mate_status done(hipError_t e) { return e == hipSuccess ? MATE_OK : MATE_ERR_HIP; }
+}  // namespace
+
+mate_status mate_linear(const void* x, const void* w, const float* bias, const uint8_t* flags,
+                        const void* residual, int B, int N, int E, int F, mate_activation act,
+                        mate_dtype t, void* y, void* z, uint8_t* z_scales, uint8_t* y_codes,
+                        uint8_t* y_scales, void* stream) {
+  if (!x || !w || !y || (z_scales && !z) || !y_codes != !y_scales) return MATE_ERR_NULL;
+  if (!tokens_ok(B, N) || E < 1 || F < 1) return MATE_ERR_SHAPE;
+  if (t != MATE_BF16 || !width_ok(E) || !width_ok(F) || !act_ok(act) || !aligned({x, w, bias, residual, y, z, y_codes})) return MATE_ERR_UNSUPPORTED;
+  const LinearCall c = {x, w, bias, flags, residual, B * N, E, F, act, y, z, z_scales, y_codes, y_scales};
+  return done(launch_linear(c, static_cast<hipStream_t>(stream)));
+}
+
+size_t mate_linear_bwd_workspace_bytes(int B, int N, int E, int F, int x_in_codes) {
+  if (!tokens_ok(B, N) || !width_ok(E) || !width_ok(F)) return 0;
+  return linear_bwd_workspace(B * N, E, F, x_in_codes != 0);
+}
+
+mate_status mate_linear_bwd(const void* dy, const void* x, const uint8_t* x_scales, const void* w,
+                            const uint8_t* flags, const void* z, const uint8_t* z_scales,
+                            const void* residual, int B, int N, int E, int F, mate_activation act,
+                            mate_dtype t, void* dx, float* dw, float* dbias, void* workspace,
+                            size_t workspace_bytes, void* stream) {
+  if (!dy || (dw && !x) || (dx && !w) || (dbias && !dw) || (z_scales && !z) || (x_scales && !x)) return MATE_ERR_NULL;
+  if (!tokens_ok(B, N) || E < 1 || F < 1) return MATE_ERR_SHAPE;
+  if (t != MATE_BF16 || !width_ok(E) || !width_ok(F) || !act_ok(act) || (act == MATE_ACT_NONE) != (z == nullptr) ||
+      !aligned({dy, x, w, z, residual, dx, dw, dbias}))
+    return MATE_ERR_UNSUPPORTED;
+  if (dw && (!workspace || workspace_bytes < linear_bwd_workspace(B * N, E, F, x_scales != nullptr))) return MATE_ERR_WORKSPACE;
+  const LinearBwdCall c = {dy, x, x_scales, w, flags, z, z_scales, residual, B * N, E, F, act, dx, dw, dbias, workspace};
+  return done(launch_linear_bwd(c, static_cast<hipStream_t>(stream)));
+}
+
+mate_status mate_activation_bwd(const void* dy, const void* z, const uint8_t* z_scales,
+                                const uint8_t* flags, int B, int N, int E, mate_activation act,
+                                mate_dtype t, void* dz, void* stream) {
+  if (!dy || !z || !dz) return MATE_ERR_NULL;
+  if (!tokens_ok(B, N) || E < 1) return MATE_ERR_SHAPE;
+  if (t != MATE_BF16 || !width_ok(E) || !act_ok(act) || act == MATE_ACT_NONE || !aligned({dy, z, dz})) return MATE_ERR_UNSUPPORTED;
+  return done(launch_activation_bwd(dy, z, z_scales, flags, B * N, E, act, dz, static_cast<hipStream_t>(stream)));
+}
+
+mate_status mate_checkpoint_pack(const void* x, const uint8_t* flags, int B, int N, int E,
+                                 mate_dtype t, uint8_t* codes, uint8_t* scales, void* stream) {
+  if (!x || !codes || !scales) return MATE_ERR_NULL;
+  if (!tokens_ok(B, N) || E < 1) return MATE_ERR_SHAPE;
+  if ((t != MATE_BF16 && t != MATE_F32) || !width_ok(E) || !aligned({x, codes})) return MATE_ERR_UNSUPPORTED;
+  return done(launch_checkpoint_pack(x, flags, B * N, E, t == MATE_F32, codes, scales, static_cast<hipStream_t>(stream)));
+}
+
+mate_status mate_checkpoint_unpack(const uint8_t* codes, const uint8_t* scales, int B, int N, int E,
+                                   mate_dtype t, void* x, void* stream) {
+  if (!x || !codes || !scales) return MATE_ERR_NULL;
+  if (!tokens_ok(B, N) || E < 1) return MATE_ERR_SHAPE;
+  if ((t != MATE_BF16 && t != MATE_F32) || !width_ok(E) || !aligned({x, codes})) return MATE_ERR_UNSUPPORTED;
+  return done(launch_checkpoint_unpack(codes, scales, B * N, E, t == MATE_F32, x, static_cast<hipStream_t>(stream)));
+}
+
 mate_status mate_attn_fwd(const void* q, const void* k, const void* v, const void* segments,
                           const uint8_t* head_kind, int B, int H, int N, int D, mate_dtype t,
                           float scale, void* out, float* lse, void* workspace,
@@ -474,7 +549,7 @@ const char* mate_status_string(mate_status s) {
     case MATE_OK: return "ok";
     case MATE_ERR_NULL: return "a required pointer is NULL";
     case MATE_ERR_SHAPE: return "shape out of range, or segment tables built for another (B, N)";
-    case MATE_ERR_UNSUPPORTED: return "unsupported head size, dtype or head kind";
+    case MATE_ERR_UNSUPPORTED: return "unsupported head size, dtype or head kind, or width, activation or address";
     case MATE_ERR_WORKSPACE: return "workspace too small or not aligned";
     case MATE_ERR_BAD_ID: return "negative id on a table token, or flag value above 2";
     case MATE_ERR_HIP: return "HIP call or kernel launch failed";

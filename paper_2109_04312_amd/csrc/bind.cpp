@@ -15,10 +15,12 @@
 #include <ATen/hip/impl/HIPStreamMasqueradingAsCUDA.h>
 #include <ATen/ops/empty.h>
 #include <ATen/ops/empty_like.h>
+#include <c10/core/DeviceGuard.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <algorithm>
+#include <array>
 #include <cstring>
 
 #include "../../include/mate.h"
@@ -31,7 +33,8 @@ namespace {
   X(mate_build_segments_bucketed) X(mate_cell_positions) X(mate_attn_fwd) X(mate_attn_bwd)        \
   X(mate_dense_workspace_bytes) X(mate_attn_fwd_dense) X(mate_attn_bwd_dense) X(mate_qkv_project) \
   X(mate_out_project) X(mate_project_bwd_workspace_bytes) X(mate_qkv_project_bwd)                 \
-  X(mate_out_project_bwd)
+  X(mate_out_project_bwd) X(mate_linear) X(mate_linear_bwd_workspace_bytes) X(mate_linear_bwd)                \
+  X(mate_activation_bwd) X(mate_checkpoint_pack) X(mate_checkpoint_unpack)
 struct Abi {
 #define X(name) decltype(&::name) name;
   MATE_FUNCTIONS(X)
@@ -39,7 +42,9 @@ struct Abi {
 } abi;
 PyObject* mate_error;                    // mate.MateError
 PyObject* to_head_kinds;                 // mate._head_kind_host
+PyObject* checkpoint_type;               // mate.Checkpoint
 PyObject *s_buf, *s_B, *s_N;             // attribute names of mate.Segments
+PyObject *s_codes, *s_scales;            // and of mate.Checkpoint
 
 // ---- errors: thrown as C++ exceptions below, turned into Python ones in guarded() --------------
 struct PyFailure {};                     // a Python exception is already set
@@ -416,7 +421,254 @@ PyObject* out_project_bwd(Args a) {  // o, w_o, flags, dy, want_do, want_dw, wan
   return pack({d_o, dw, db});
 }
 
-PyObject* bind(Args a) {  // {name: address}, MateError, _head_kind_host
+// ---- the feed-forward half: every tensor is checked (a wrong one would be read past its end), and the calls run on the first one's
+// device and on that device's current stream ----
+struct OnDevice {
+  c10::DeviceGuard guard;
+  c10::Device device;
+  explicit OnDevice(const at::Tensor& t) : guard(t.device()), device(t.device()) {
+    if (!t.is_cuda()) fail(PyExc_ValueError, "expected device tensors");
+  }
+  void* stream() const { return c10::hip::getCurrentHIPStreamMasqueradingAsCUDA(device.index()).stream(); }
+  // t's address; its type, shape and place are as expected
+  void* of(const at::Tensor& t, at::ScalarType type, at::IntArrayRef shape, const char* name) const {
+    if (t.scalar_type() != type) {
+      PyErr_Format(PyExc_TypeError, "%s must be of type %s, not %s", name, c10::toString(type), c10::toString(t.scalar_type()));
+      throw PyFailure();
+    }
+    if (t.sizes() != shape) {
+      PyErr_Format(PyExc_ValueError, "%s has another shape than the other tensors ask for", name);
+      throw PyFailure();
+    }
+    void* p = dev(t, name);
+    if (t.device() != device) {
+      PyErr_Format(PyExc_ValueError, "%s is on another device", name);
+      throw PyFailure();
+    }
+    return p;
+  }
+  void* of(PyObject* o, at::ScalarType type, at::IntArrayRef shape, const char* name) const {
+    return o == Py_None ? nullptr : of(tensor(o, name), type, shape, name);
+  }
+};
+// [B, N, W] of a token tensor
+struct Tokens {
+  int B, N, W;
+  Tokens(const at::Tensor& t, const char* name) {
+    if (t.dim() != 3) {
+      PyErr_Format(PyExc_ValueError, "%s must have shape [B, N, width]", name);
+      throw PyFailure();
+    }
+    B = size(t, 0), N = size(t, 1), W = size(t, 2);
+  }
+  static int size(const at::Tensor& t, int d) { return (int)std::min<int64_t>(t.size(d), 2147483647); }
+  std::array<int64_t, 3> with(int64_t width) const { return {B, N, width}; }
+  std::array<int64_t, 3> scales(int64_t width) const { return {B, N, (width + MATE_SCALE_BLOCK - 1) / MATE_SCALE_BLOCK}; }
+};
+// The two tensors of a mate.Checkpoint of [B, N, width] values, or of None.
+struct Codes {
+  at::Tensor codes, scales;
+  uint8_t *code = nullptr, *scale = nullptr;
+  explicit operator bool() const { return code; }
+  Codes() = default;
+  Codes(PyObject* o, const OnDevice& d, const Tokens& x, int width, const char* name) {
+    PyObject *c = PyObject_GetAttr(o, s_codes), *s = c ? PyObject_GetAttr(o, s_scales) : nullptr;
+    if (!s) {
+      Py_XDECREF(c);
+      throw PyFailure();
+    }
+    const bool tensors = THPVariable_Check(c) && THPVariable_Check(s);
+    if (tensors) {
+      codes = THPVariable_Unpack(c);
+      scales = THPVariable_Unpack(s);
+    }
+    Py_DECREF(c);
+    Py_DECREF(s);
+    if (!tensors) fail(PyExc_TypeError, "a checkpoint holds two tensors");
+    place(d, x, width, name);
+  }
+  static Codes fresh(const OnDevice& d, const Tokens& x, int width, const at::Tensor& like) {
+    Codes k;
+    k.codes = at::empty(x.with(width), at::TensorOptions(like.device()).dtype(at::kByte));
+    k.scales = at::empty(x.scales(width), at::TensorOptions(like.device()).dtype(at::kByte));
+    k.place(d, x, width, "checkpoint");
+    return k;
+  }
+  void place(const OnDevice& d, const Tokens& x, int width, const char* name) {
+    code = (uint8_t*)d.of(codes, at::kByte, x.with(width), name);
+    scale = (uint8_t*)d.of(scales, at::kByte, x.scales(width), name);
+  }
+  PyObject* wrap() const {
+    PyObject *c = THPVariable_Wrap(codes), *s = c ? THPVariable_Wrap(scales) : nullptr;
+    PyObject* r = s ? PyObject_CallFunctionObjArgs(checkpoint_type, c, s, nullptr) : nullptr;
+    Py_XDECREF(c);
+    Py_XDECREF(s);
+    if (!r) throw PyFailure();
+    return r;
+  }
+};
+bool is_codes(PyObject* o) {
+  const int v = PyObject_IsInstance(o, checkpoint_type);
+  if (v < 0) throw PyFailure();
+  return v != 0;
+}
+// A kept activation of [B, N, width]: bf16, or codes and scales.
+struct Kept {
+  Codes codes;
+  const void* p = nullptr;
+  const uint8_t* scales = nullptr;
+  Kept(PyObject* o, const OnDevice& d, const Tokens& x, int width, const char* name) {
+    if (o == Py_None) return;
+    if (is_codes(o)) {
+      codes = Codes(o, d, x, width, name);
+      p = codes.code;
+      scales = codes.scale;
+    } else {
+      p = d.of(o, at::kBFloat16, x.with(width), name);
+    }
+  }
+};
+PyObject* wrap_or_none(const at::Tensor& t) {
+  if (t.defined()) return THPVariable_Wrap(t);
+  Py_RETURN_NONE;
+}
+PyObject* tuple_of(std::initializer_list<PyObject*> items) {   // steals the references
+  PyObject* r = PyTuple_New((Py_ssize_t)items.size());
+  bool whole = r != nullptr;
+  Py_ssize_t i = 0;
+  for (PyObject* o : items) {
+    whole = whole && o;
+    if (r) PyTuple_SET_ITEM(r, i++, o);
+    else Py_XDECREF(o);
+  }
+  if (!whole) {
+    Py_XDECREF(r);
+    throw PyFailure();
+  }
+  return r;
+}
+
+PyObject* linear(Args a) {  // x, w, bias, flags, act, residual, keep_z, keep_y, y
+  const at::Tensor &x = tensor(a[0], "x"), &w = tensor(a[1], "w");
+  const Tokens s(x, "x");
+  if (w.dim() != 2) fail(PyExc_ValueError, "w must have shape [F, E]");
+  const int E = s.W, F = Tokens::size(w, 0), act = integer(a[4]), keep_z = integer(a[6]);
+  if (keep_z < 0 || keep_z > 2) fail(PyExc_ValueError, "keep_z must be MATE_KEEP_NONE, MATE_KEEP_BF16 or MATE_KEEP_8BIT");
+  const bool keep_y = truth(a[7]);
+  const OnDevice d(x);
+  void *px = d.of(x, at::kBFloat16, s.with(E), "x"), *pw = d.of(w, at::kBFloat16, {F, E}, "w"),
+       *pb = d.of(a[2], at::kFloat, {F}, "bias"), *pf = d.of(a[3], at::kByte, {s.B, s.N}, "flags"),
+       *pr = d.of(a[5], at::kBFloat16, s.with(F), "residual");
+  const at::Tensor y = a[8] == Py_None ? new_tensor({s.B, s.N, F}, at::kBFloat16, x) : tensor(a[8], "y");
+  void* py = d.of(y, at::kBFloat16, s.with(F), "y");
+  at::Tensor z;
+  void* pz = nullptr;
+  Codes z8, y8;
+  if (keep_z == 1) {
+    z = new_tensor({s.B, s.N, F}, at::kBFloat16, x);
+    pz = z.data_ptr();
+  } else if (keep_z == 2) {
+    z8 = Codes::fresh(d, s, F, x);
+    pz = z8.code;
+  }
+  if (keep_y) y8 = Codes::fresh(d, s, F, x);
+  void* st = d.stream();
+  call("mate_linear", [&] {
+    return abi.mate_linear(px, pw, (const float*)pb, (uint8_t*)pf, pr, s.B, s.N, E, F, (mate_activation)act, MATE_BF16, py, pz, z8.scale, y8.code,
+                           y8.scale, st);
+  });
+  PyObject* kept = z8 ? z8.wrap() : wrap_or_none(z);
+  if (!keep_y) return tuple_of({THPVariable_Wrap(y), kept});
+  PyObject* kept_y;
+  try {
+    kept_y = y8.wrap();
+  } catch (...) {
+    Py_XDECREF(kept);
+    throw;
+  }
+  return tuple_of({THPVariable_Wrap(y), kept, kept_y});
+}
+
+PyObject* linear_bwd(Args a) {  // dy, x, w, flags, z, act, residual, want_dx, want_dw, want_dbias, ws
+  const at::Tensor &dy = tensor(a[0], "dy"), &w = tensor(a[2], "w");
+  const Tokens s(dy, "dy");
+  if (w.dim() != 2) fail(PyExc_ValueError, "w must have shape [F, E]");
+  const int F = s.W, E = Tokens::size(w, 1), act = integer(a[5]);
+  const bool want_dx = truth(a[7]), want_dw = truth(a[8]), want_db = truth(a[9]);
+  const OnDevice d(dy);
+  void *pg = d.of(dy, at::kBFloat16, s.with(F), "dy"), *pw = d.of(w, at::kBFloat16, {F, E}, "w"), *pf = d.of(a[3], at::kByte, {s.B, s.N}, "flags"),
+       *pr = d.of(a[6], at::kBFloat16, s.with(E), "residual");
+  const Kept x(a[1], d, s, E, "x"), z(a[4], d, s, E, "z");
+  at::Tensor dx, dw, db;
+  if (want_dx) dx = new_tensor({s.B, s.N, E}, at::kBFloat16, dy);
+  if (want_dw) dw = new_tensor({F, E}, at::kFloat, dy);
+  if (want_db) db = new_tensor({F}, at::kFloat, dy);
+  at::Tensor ws;
+  if (want_dw) {
+    const size_t need = abi.mate_linear_bwd_workspace_bytes(s.B, s.N, E, F, x.scales != nullptr);
+    if (a[10] == Py_None) ws = new_tensor({(int64_t)std::max<size_t>(need, 16)}, at::kByte, dy);
+    else {
+      ws = tensor(a[10], "ws");
+      d.of(ws, at::kByte, ws.sizes(), "ws");
+    }
+  }
+  void *pdx = want_dx ? dx.data_ptr() : nullptr, *pdw = want_dw ? dw.data_ptr() : nullptr, *pdb = want_db ? db.data_ptr() : nullptr,
+       *pws = want_dw ? ws.data_ptr() : nullptr;
+  const size_t ws_bytes = want_dw ? (size_t)ws.numel() : 0;
+  void* st = d.stream();
+  call("mate_linear_bwd", [&] {
+    return abi.mate_linear_bwd(pg, x.p, x.scales, pw, (uint8_t*)pf, z.p, z.scales, pr, s.B, s.N, E, F, (mate_activation)act, MATE_BF16, pdx,
+                               (float*)pdw, (float*)pdb, pws, ws_bytes, st);
+  });
+  return pack({dx, dw, db});
+}
+
+PyObject* activation_bwd(Args a) {  // dy, z, act, flags, dz
+  const at::Tensor& dy = tensor(a[0], "dy");
+  const Tokens s(dy, "dy");
+  const int act = integer(a[2]);
+  const OnDevice d(dy);
+  void *pg = d.of(dy, at::kBFloat16, s.with(s.W), "dy"), *pf = d.of(a[3], at::kByte, {s.B, s.N}, "flags");
+  const Kept z(a[1], d, s, s.W, "z");
+  at::Tensor dz = a[4] == Py_None ? new_tensor({s.B, s.N, s.W}, at::kBFloat16, dy) : tensor(a[4], "dz");
+  void *pz = d.of(dz, at::kBFloat16, s.with(s.W), "dz"), *st = d.stream();
+  call("mate_activation_bwd", [&] {
+    return abi.mate_activation_bwd(pg, z.p, z.scales, (uint8_t*)pf, s.B, s.N, s.W, (mate_activation)act, MATE_BF16, pz, st);
+  });
+  return THPVariable_Wrap(std::move(dz));
+}
+
+PyObject* checkpoint_pack(Args a) {  // x, flags, out
+  const at::Tensor& x = tensor(a[0], "x");
+  const Tokens s(x, "x");
+  const mate_dtype t = dtype_code(x);
+  const OnDevice d(x);
+  void *px = d.of(x, x.scalar_type(), s.with(s.W), "x"), *pf = d.of(a[1], at::kByte, {s.B, s.N}, "flags");
+  const Codes k = a[2] == Py_None ? Codes::fresh(d, s, s.W, x) : Codes(a[2], d, s, s.W, "out");
+  void* st = d.stream();
+  call("mate_checkpoint_pack", [&] { return abi.mate_checkpoint_pack(px, (uint8_t*)pf, s.B, s.N, s.W, t, k.code, k.scale, st); });
+  if (a[2] == Py_None) return k.wrap();
+  Py_INCREF(a[2]);
+  return a[2];
+}
+
+PyObject* checkpoint_unpack(Args a) {  // checkpoint, f32, out
+  PyObject* c = PyObject_GetAttr(a[0], s_codes);
+  if (!c) throw PyFailure();
+  Py_DECREF(c);  // (the checkpoint holds it)
+  const at::Tensor& codes = tensor(c, "codes");
+  const Tokens s(codes, "codes");
+  const at::ScalarType type = truth(a[1]) ? at::kFloat : at::kBFloat16;
+  const OnDevice d(codes);
+  const Codes k(a[0], d, s, s.W, "checkpoint");
+  at::Tensor x = a[2] == Py_None ? new_tensor({s.B, s.N, s.W}, type, codes) : tensor(a[2], "out");
+  void *px = d.of(x, type, s.with(s.W), "out"), *st = d.stream();
+  call("mate_checkpoint_unpack",
+       [&] { return abi.mate_checkpoint_unpack(k.code, k.scale, s.B, s.N, s.W, type == at::kFloat ? MATE_F32 : MATE_BF16, px, st); });
+  return THPVariable_Wrap(std::move(x));
+}
+
+PyObject* bind(Args a) {  // {name: address}, MateError, _head_kind_host, Checkpoint
 #define X(name)                                                              \
   {                                                                          \
     PyObject* v = PyDict_GetItemString(a[0], #name);                         \
@@ -431,6 +683,8 @@ PyObject* bind(Args a) {  // {name: address}, MateError, _head_kind_host
   mate_error = a[1];
   Py_INCREF(a[2]);
   to_head_kinds = a[2];
+  Py_INCREF(a[3]);
+  checkpoint_type = a[3];
   Py_RETURN_NONE;
 }
 
@@ -450,11 +704,12 @@ PyObject* guarded(PyObject*, PyObject* const* args, Py_ssize_t n) {
 }
 
 #define METHOD(name, n) {#name, (PyCFunction)(void (*)())guarded<name, n>, METH_FASTCALL, nullptr}
-PyMethodDef methods[] = {METHOD(bind, 3),           METHOD(build_segments, 6),  METHOD(segments_buffer, 1),
+PyMethodDef methods[] = {METHOD(bind, 4),           METHOD(build_segments, 6),  METHOD(segments_buffer, 1),
                          METHOD(cell_positions, 4), METHOD(attn_fwd, 9),        METHOD(attn_bwd, 13),
                          METHOD(attn_fwd_dense, 10), METHOD(attn_bwd_dense, 15), METHOD(qkv_project, 8),
                          METHOD(out_project, 5),    METHOD(qkv_project_bwd, 10), METHOD(out_project_bwd, 8),
-                         {nullptr, nullptr, 0, nullptr}};
+                         METHOD(linear, 9),         METHOD(linear_bwd, 11),     METHOD(activation_bwd, 5),   METHOD(checkpoint_pack, 3),
+                         METHOD(checkpoint_unpack, 3), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", "Tensor-level calls of the C ABI (see mate.py).", -1, methods};
 
 }  // namespace
@@ -463,5 +718,7 @@ PyMODINIT_FUNC PyInit__native() {
   s_buf = PyUnicode_InternFromString("buf");
   s_B = PyUnicode_InternFromString("B");
   s_N = PyUnicode_InternFromString("N");
+  s_codes = PyUnicode_InternFromString("codes");
+  s_scales = PyUnicode_InternFromString("scales");
   return PyModule_Create(&module);
 }

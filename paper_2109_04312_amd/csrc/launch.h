@@ -125,6 +125,38 @@ hipError_t launch_out_project_bwd(const void* o, const void* w_o, const unsigned
                                   const void* dy, int B, int N, int H, int E, void* d_o, float* dw,
                                   float* dbias, void* workspace, unsigned long long ticket, hipStream_t stream);
 
+// The feed-forward half (bf16; T flat tokens, widths multiples of 8; see mate.h).  *_scales null: that tensor is bf16, else codes.
+struct LinearCall {
+  const void *x, *w;
+  const float* bias;
+  const unsigned char* flags;
+  const void* residual;
+  int T, E, F, act;
+  void *y, *z;
+  unsigned char *z_scales, *y_codes, *y_scales;
+};
+hipError_t launch_linear(const LinearCall& c, hipStream_t stream);
+struct LinearBwdCall {
+  const void *dy, *x;
+  const unsigned char* x_scales;
+  const void* w;
+  const unsigned char* flags;
+  const void* z;
+  const unsigned char* z_scales;
+  const void* residual;
+  int T, E, F, act;
+  void* dx;
+  float *dw, *dbias;
+  void* workspace;
+};
+size_t linear_bwd_workspace(int T, int E, int F, bool codes);
+hipError_t launch_linear_bwd(const LinearBwdCall& c, hipStream_t stream);
+hipError_t launch_activation_bwd(const void* dy, const void* z, const unsigned char* z_scales, const unsigned char* flags, int rows, int E, int act,
+                                 void* dz, hipStream_t stream);
+hipError_t launch_checkpoint_pack(const void* x, const unsigned char* flags, int rows, int E, bool f32, unsigned char* codes, unsigned char* scales,
+                                  hipStream_t stream);
+hipError_t launch_checkpoint_unpack(const unsigned char* codes, const unsigned char* scales, int rows, int E, bool f32, void* x, hipStream_t stream);
+
 // Measurement aid: `workgroups` x 4 wavefronts each issue `iters` x 8 independent 32x32x16 bf16
 // MFMAs and write one float per thread to `sink` (workgroups * 256 floats).
 hipError_t launch_mfma_probe(float* sink, int workgroups, int iters, hipStream_t stream);

@@ -28,7 +28,8 @@ MATE_MAX_N, MATE_MAX_HEADS, MATE_HEAD_DIM = 16384, 256, 64
 
 EXPORTS = ["mate_segments_bytes", "mate_workspace_bytes", "mate_build_segments",
            "mate_build_segments_bucketed", "mate_cell_positions", "mate_segments_export", "mate_segments_export_windows", "mate_attn_fwd", "mate_attn_bwd", "mate_dense_workspace_bytes",
-           "mate_attn_fwd_dense", "mate_attn_bwd_dense", "mate_attn_bwd_dense_static", "mate_attn_prefers_dense", "mate_segments_status", "mate_qkv_project", "mate_out_project", "mate_project_bwd_workspace_bytes", "mate_qkv_project_bwd", "mate_out_project_bwd", "mate_profile_kernel",
+           "mate_attn_fwd_dense", "mate_attn_bwd_dense", "mate_attn_bwd_dense_static", "mate_attn_prefers_dense", "mate_segments_status", "mate_qkv_project", "mate_out_project", "mate_project_bwd_workspace_bytes", "mate_qkv_project_bwd", "mate_out_project_bwd",
+           "mate_linear", "mate_linear_bwd_workspace_bytes", "mate_linear_bwd", "mate_activation_bwd", "mate_checkpoint_pack", "mate_checkpoint_unpack", "mate_profile_kernel",
            "mate_probe_mfma", "mate_status_string"]
 MATE_KERNEL_NONE, MATE_KERNEL_BUILD, MATE_KERNEL_FWD = 0, 1, 2
 MATE_KERNEL_BWD_DQ, MATE_KERNEL_BWD_DKV = 3, 4
@@ -36,6 +37,9 @@ MATE_KERNEL_FWD_DENSE, MATE_KERNEL_BWD_DQ_DENSE, MATE_KERNEL_BWD_DKV_DENSE = 5, 
 MATE_KERNEL_QKV_PROJECT, MATE_KERNEL_OUT_PROJECT = 8, 9
 MATE_KERNEL_QKV_PROJECT_DGRAD, MATE_KERNEL_QKV_PROJECT_WGRAD = 10, 11
 MATE_KERNEL_OUT_PROJECT_DGRAD, MATE_KERNEL_OUT_PROJECT_WGRAD = 12, 13
+MATE_ACT_NONE, MATE_ACT_RELU, MATE_ACT_GELU, MATE_ACT_GELU_TANH, MATE_ACT_SILU, MATE_ACT_TANH = 0, 1, 2, 3, 4, 5
+MATE_SCALE_BLOCK, MATE_MAX_WIDTH = 32, 65536
+MATE_KEEP_NONE, MATE_KEEP_BF16, MATE_KEEP_8BIT = 0, 1, 2   # how linear() keeps its pre-activation
 MATE_DENSE_MAX_N = 1024
 MATE_DENSE_PREFERRED_MAX_N = 256
 
@@ -92,6 +96,18 @@ _lib.mate_qkv_project_bwd.restype = _i
 _lib.mate_qkv_project_bwd.argtypes = [_p, _p, _p, _p, _p, _p, _i, _i, _i, _i, _i, _p, _p, _p, _p, _sz, _p]
 _lib.mate_out_project_bwd.restype = _i
 _lib.mate_out_project_bwd.argtypes = [_p, _p, _p, _p, _i, _i, _i, _i, _i, _p, _p, _p, _p, _sz, _p]
+_lib.mate_linear.restype = _i
+_lib.mate_linear.argtypes = [_p, _p, _p, _p, _p, _i, _i, _i, _i, _i, _i, _p, _p, _p, _p, _p, _p]
+_lib.mate_linear_bwd_workspace_bytes.restype = _sz
+_lib.mate_linear_bwd_workspace_bytes.argtypes = [_i, _i, _i, _i, _i]
+_lib.mate_linear_bwd.restype = _i
+_lib.mate_linear_bwd.argtypes = [_p, _p, _p, _p, _p, _p, _p, _p, _i, _i, _i, _i, _i, _i, _p, _p, _p, _p, _sz, _p]
+_lib.mate_activation_bwd.restype = _i
+_lib.mate_activation_bwd.argtypes = [_p, _p, _p, _p, _i, _i, _i, _i, _i, _p, _p]
+_lib.mate_checkpoint_pack.restype = _i
+_lib.mate_checkpoint_pack.argtypes = [_p, _p, _i, _i, _i, _i, _p, _p, _p]
+_lib.mate_checkpoint_unpack.restype = _i
+_lib.mate_checkpoint_unpack.argtypes = [_p, _p, _i, _i, _i, _i, _p, _p]
 _lib.mate_profile_kernel.restype = _i
 _lib.mate_profile_kernel.argtypes = [_i, _p, _p]
 _lib.mate_probe_mfma.restype = _i
@@ -122,6 +138,12 @@ mate_out_project = _lib.mate_out_project
 mate_project_bwd_workspace_bytes = _lib.mate_project_bwd_workspace_bytes
 mate_qkv_project_bwd = _lib.mate_qkv_project_bwd
 mate_out_project_bwd = _lib.mate_out_project_bwd
+mate_linear = _lib.mate_linear
+mate_linear_bwd_workspace_bytes = _lib.mate_linear_bwd_workspace_bytes
+mate_linear_bwd = _lib.mate_linear_bwd
+mate_activation_bwd = _lib.mate_activation_bwd
+mate_checkpoint_pack = _lib.mate_checkpoint_pack
+mate_checkpoint_unpack = _lib.mate_checkpoint_unpack
 
 
 def mate_status_string(status: int) -> str:
@@ -151,13 +173,20 @@ class Segments:
     N: int
 
 
+@dataclass
+class Checkpoint:
+    """[B, N, W] activations in 8 bits: e4m3 codes [B, N, W] and scales [B, N, ceil(W / 32)], both uint8."""
+    codes: torch.Tensor
+    scales: torch.Tensor
+
+
 def _head_kind_host(head_kind, H: int):
     hk = np.ascontiguousarray(np.asarray(head_kind, dtype=np.uint8))
     assert hk.shape == (H,)
     return hk
 
 
-_native.bind({n: C.cast(getattr(_lib, n), C.c_void_p).value for n in EXPORTS}, MateError, _head_kind_host)
+_native.bind({n: C.cast(getattr(_lib, n), C.c_void_p).value for n in EXPORTS}, MateError, _head_kind_host, Checkpoint)
 
 
 def build_segments(row_ids: torch.Tensor, col_ids: torch.Tensor, flags: torch.Tensor,
@@ -243,6 +272,45 @@ def qkv_project_bwd(x, w_qkv, flags, dq, dk, dv, want_dx=True, want_dw=True, wan
 def out_project_bwd(o, w_o, flags, dy, want_do=True, want_dw=True, want_dbias=True, ws=None):
     """Gradients of out_project: d_o [B,H,N,64] bf16, dw_o [E,H*64] float32, dbias [E] float32."""
     return _native.out_project_bwd(o, w_o, flags, dy, want_do, want_dw, want_dbias, ws)
+
+
+def linear(x, w, bias=None, flags=None, act=MATE_ACT_NONE, residual=None, keep_z=MATE_KEEP_NONE, keep_y=False, y=None):
+    """z = x w^T + bias, y = act(z) + residual: x [B,N,E] bf16, w [F,E] bf16, bias [F] float32 or None, residual [B,N,F] bf16
+    or None (it may be y) -> (y [B,N,F] bf16, z), z for the backward as keep_z says: None, bf16 or a Checkpoint.  keep_y: a third
+    result, y as a Checkpoint, for the backward of the product that reads y."""
+    return _native.linear(x, w, bias, flags, act, residual, keep_z, keep_y, y)
+
+
+def linear_bwd_workspace(B, N, E, F, x_in_codes, device) -> torch.Tensor:
+    n = mate_linear_bwd_workspace_bytes(B, N, E, F, int(x_in_codes))
+    if n == 0:
+        raise MateError(MATE_ERR_UNSUPPORTED, "mate_linear_bwd_workspace_bytes")
+    return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+def linear_bwd(dy, x, w, flags=None, z=None, act=MATE_ACT_NONE, residual=None, want_dx=True, want_dw=True, want_dbias=True, ws=None):
+    """Gradients of linear() at its pre-activation, dy [B,N,F] bf16: dx = (dy w) act'(z) + residual [B,N,E] bf16, dw = sum dy^T x
+    [F,E] float32, dbias [F] float32 (None for the ones not wanted).  x (bf16 or a Checkpoint; None if dw is not wanted) is what
+    the product read; if that was an activation, x = act(z), z (bf16 or a Checkpoint) makes dx the gradient at z.  residual: a
+    gradient that reached x on another way."""
+    return _native.linear_bwd(dy, x, w, flags, z, act, residual, want_dx, want_dw, want_dbias, ws)
+
+
+def activation_bwd(dy, z, act, flags=None, dz=None):
+    """dz = dy act'(z), z bf16 or a Checkpoint [B,N,W], for an activation that no product follows (dz may be dy)."""
+    return _native.activation_bwd(dy, z, act, flags, dz)
+
+
+def checkpoint_pack(x, flags=None, out: Checkpoint | None = None) -> Checkpoint:
+    """x [B,N,W] bf16 or float32 in 8 bits; rows of padding as zeros."""
+    return _native.checkpoint_pack(x, flags, out)
+
+
+def checkpoint_unpack(checkpoint: Checkpoint, dtype: torch.dtype = torch.bfloat16, out=None) -> torch.Tensor:
+    """The values that a checkpoint stands for, bf16 or float32 (either holds them exactly)."""
+    if dtype not in (torch.bfloat16, torch.float32):
+        raise TypeError(f"unsupported dtype {dtype}")
+    return _native.checkpoint_unpack(checkpoint, dtype == torch.float32, out)
 
 
 def prefer_dense(B: int, H: int, N: int, dtype: torch.dtype = torch.bfloat16) -> bool:
