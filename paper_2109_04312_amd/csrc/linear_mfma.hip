@@ -42,15 +42,247 @@ struct LinearArgs : LinearStart {
   unsigned short* y;            // [T][O]
   void* z;                      // forward: bf16, or codes if z_scales is not null; or null
   unsigned char *z_scales, *y_codes, *y_scales;
+  int far;                      // y passes the memory-side cache
   RangeSums ranges;
 };
 
-// Eight consecutive features of a token, in two words of codes or four of bf16, and a lane's four features of each block of a pair in the
-// accumulators' layout: exchanging quarters between the two blocks' words turns one into the other, both ways.
-struct Pair { unsigned u[2]; };
-__device__ __forceinline__ Pair exchange(unsigned x, unsigned y) {
-  const auto r = __builtin_amdgcn_permlane16_swap(x, y, false, false);
-  return {{r[0], r[1]}};
+// ---- epilogue ------------------------------------------------------------------------------------
+// A wavefront's part of a token tensor: rows of its tokens from its first feature on.  Lanes past the last token or feature read zeros and
+// write nothing, by the range that the hardware checks, so that no branch stands around an access: the compiler
+// counts what is under way, and waits for a read and not for the writes behind it.
+struct Part {
+  __amdgpu_buffer_rsrc_t rsrc;
+  __device__ __forceinline__ Part(const void* p, int bytes_each, int width, int t_first, int f_first, int T)
+      : rsrc(__builtin_amdgcn_make_buffer_rsrc(
+            const_cast<char*>(uniform_ptr(static_cast<const char*>(p) + ((size_t)t_first * width + f_first) * bytes_each)), 0,
+            p ? __builtin_amdgcn_readfirstlane((min(T - t_first, 64) * width - f_first) * bytes_each) : 0, 0x00027000)) {}
+  __device__ __forceinline__ u32x4 load16(unsigned at) const { return __builtin_amdgcn_raw_buffer_load_b128(rsrc, at, 0, 0); }
+  __device__ __forceinline__ uint2 load8(unsigned at) const {
+    const auto v = __builtin_amdgcn_raw_buffer_load_b64(rsrc, at, 0, 0);
+    return make_uint2(v[0], v[1]);
+  }
+  __device__ __forceinline__ unsigned load1(unsigned at) const { return __builtin_amdgcn_raw_buffer_load_b8(rsrc, at, 0, 0); }
+  template <int kAux = 0>
+  __device__ __forceinline__ void store16(unsigned at, u32x4 v) const { __builtin_amdgcn_raw_buffer_store_b128(v, rsrc, at, 0, kAux); }
+  template <int kAux = 0>
+  __device__ __forceinline__ void store8(unsigned at, unsigned x, unsigned y) const {
+    typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
+    __builtin_amdgcn_raw_buffer_store_b64(u32x2{x, y}, rsrc, at, 0, kAux);
+  }
+  __device__ __forceinline__ void store1(unsigned at, unsigned x) const { __builtin_amdgcn_raw_buffer_store_b8((unsigned char)x, rsrc, at, 0, 0); }
+};
+constexpr unsigned kNowhere = 0x7fffffffu;   // an offset past every part's end
+constexpr int kNonTemporal = 2;
+
+// A wavefront's kFA x kNB blocks of 16 features x 16 tokens, in fp32 until a result is rounded.  They go through LDS, 16 tokens at a time
+// (kArea such chunks where there is room), so that a lane holds eight consecutive features of a token: memory is read and written 16 bytes a
+// lane, 256 of a token's bytes side by side, and four lanes hold the block of a scale.  Chunk c of 16 bytes of row r lies at slot
+// c ^ r ^ (c >> 4): both the accumulators' columns of 16 rows and rows of eight features are free of bank conflicts.
+// What is read from memory is read kAhead steps ahead, into registers that the operands no longer need.
+enum ZKind { kZNone = 0, kZBf16 = 1, kZCodes = 2 };   // of the pre-activation that is read
+template <int kFA, int kNB, int kArea, bool kGrad, int kZ, bool kAdd, int kAct>
+__device__ __forceinline__ void finish_as(const LinearStart& p, const LinearArgs& a, const f32x4 (&sum)[kFA][kNB], char* area, int t_first, int f_first) {
+  constexpr int kLanes = 2 * kFA, kTokens = 64 / kLanes, kSteps = 16 / kTokens, kRow = kFA * 64, kChunkBytes = 16 * kRow;
+  constexpr int kPhase = kArea * kSteps, kAhead = kPhase % 4 == 0 ? 4 : 2;
+  static_assert(kNB % kArea == 0 && 64 % kLanes == 0 && kPhase % kAhead == 0, "whole chunks and rows");
+  const int lane = threadIdx.x & 63, r = lane & 15, quarter = lane >> 4;
+  const int token = lane / kLanes, f_lane = 8 * (lane % kLanes), c = f_lane / 4, scales = scale_blocks(p.O);
+  const bool real = f_first + f_lane < p.O;
+  f32x4 bias[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
+  if (!kGrad && a.bias) {
+    const f32x4* b = reinterpret_cast<const f32x4*>(a.bias + min(f_first + f_lane, p.O - 8));
+    bias[0] = b[0];
+    bias[1] = b[1];
+  }
+  // Padding of the wavefront's tokens, a bit each.
+  unsigned long long pads = 0;
+  if (a.flags) pads = __ballot(a.flags[min(t_first + lane, p.T - 1)] >= 2);
+  const bool masked = pads || f_first + 16 * kFA > p.O;   // does any value not count?
+  const Part add(a.add, 2, p.O, t_first, f_first, p.T), y(a.y, 2, p.O, t_first, f_first, p.T);
+  const Part z_in(a.z_in, kZ == kZCodes ? 1 : 2, p.O, t_first, f_first, p.T), z_in_scale(a.z_in_scales, 1, scales, t_first, f_first / kScaleBlock, p.T);
+  const Part z_out(a.z, a.z_scales ? 1 : 2, p.O, t_first, f_first, p.T), z_scale(a.z_scales, 1, scales, t_first, f_first / kScaleBlock, p.T);
+  const Part y_code(a.y_codes, 1, p.O, t_first, f_first, p.T), y_scale(a.y_scales, 1, scales, t_first, f_first / kScaleBlock, p.T);
+  // Offsets of a step's values, in elements, and of its scales.
+  const unsigned at0 = real ? (unsigned)(token * p.O + f_lane) : kNowhere / 2, at_step = (unsigned)(kTokens * p.O);
+  const unsigned scale0 = real ? (unsigned)(token * scales + f_lane / kScaleBlock) : kNowhere, scale_step = (unsigned)(kTokens * scales);
+  auto at = [&](int step) { return at0 + (real ? step * at_step : 0u); };
+  auto scale_at = [&](int step) { return scale0 + (real ? step * scale_step : 0u); };
+  struct Read {
+    u32x4 add, z;
+    unsigned scale;
+  };
+  auto fetch = [&](int step) {
+    Read x;
+    if (kAdd) x.add = add.load16(2 * at(step));
+    if (kZ == kZBf16) x.z = z_in.load16(2 * at(step));
+    if (kZ == kZCodes) {
+      const uint2 w = z_in.load8(at(step));
+      x.z = u32x4{w.x, w.y, 0, 0};
+      x.scale = z_in_scale.load1(scale_at(step));
+    }
+    return x;
+  };
+  auto quad_magnitude = [](unsigned m) {
+    m = max(m, (unsigned)__builtin_amdgcn_update_dpp(0, (int)m, 0xb1, 0xf, 0xf, false));
+    return max(m, (unsigned)__builtin_amdgcn_update_dpp(0, (int)m, 0x4e, 0xf, 0xf, false));
+  };
+  const int from = token * kRow + ((c ^ token ^ (c >> 4)) << 4);
+  Read x[kAhead];
+#pragma unroll
+  for (int k = 0; k < kAhead; ++k) x[k] = fetch(k);
+#pragma unroll 1
+  for (int j0 = 0; j0 < kNB; j0 += kArea) {
+#pragma unroll
+    for (int k = 0; k < kNB; k += kArea)
+      if (k == j0) {
+#pragma unroll
+        for (int j = 0; j < kArea; ++j)
+#pragma unroll
+          for (int i = 0; i < kFA; ++i) {
+            const int c = 4 * i + quarter;
+            *reinterpret_cast<f32x4*>(area + j * kChunkBytes + r * kRow + ((c ^ r ^ (c >> 4)) << 4)) = sum[i][k + j];
+          }
+      }
+#pragma unroll 1
+    for (int s0 = 0; s0 < kPhase; s0 += kAhead) {
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k) {
+        const int step = j0 * kSteps + s0 + k;
+        // rows kTokens (step % kSteps) + token of a chunk: the step's bits and the token's do not meet
+        const int in_chunk = (s0 + k) % kSteps * kTokens;
+        const char* const chunk = area + (s0 + k) / kSteps * kChunkBytes + in_chunk * kRow;
+        const f32x4 lo = *reinterpret_cast<const f32x4*>(chunk + (from ^ (in_chunk << 4))), hi = *reinterpret_cast<const f32x4*>(chunk + (from ^ (in_chunk << 4) ^ 16));
+        const Read now = x[k];
+        float v[8], z[8];
+        if (kZ == kZCodes) {
+          const f32x4 z_lo = from_codes(now.z[0], scale_value(now.scale)), z_hi = from_codes(now.z[1], scale_value(now.scale));
+#pragma unroll
+          for (int e = 0; e < 4; ++e) { z[e] = z_lo[e]; z[4 + e] = z_hi[e]; }
+        }
+        if (kZ == kZBf16)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) { z[2 * e] = low_bf16(now.z[e]); z[2 * e + 1] = high_bf16(now.z[e]); }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const float s = e < 4 ? lo[e % 4] : hi[e % 4];
+          if constexpr (kGrad) {
+            v[e] = kZ == kZNone ? s : s * slope<kAct>(z[e]);
+          } else {
+            z[e] = s + bias[e / 4][e % 4];
+            v[e] = activate<kAct>(z[e]);
+          }
+        }
+        if (kAdd)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) { v[2 * e] += low_bf16(now.add[e]); v[2 * e + 1] += high_bf16(now.add[e]); }
+        if (masked) {
+          const bool counts = real && !((pads >> (step * kTokens + token)) & 1);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            v[e] = counts ? v[e] : 0.f;
+            if (!kGrad) z[e] = counts ? z[e] : 0.f;
+          }
+        }
+        x[k] = fetch(step + kAhead);   // (past the last step: zeros)
+        auto words = [](const float (&x)[8]) { return u32x4{pack2(x[0], x[1]), pack2(x[2], x[3]), pack2(x[4], x[5]), pack2(x[6], x[7])}; };
+        auto store_8bit = [&](const Part& codes, const Part& scales_of, float (&x)[8]) {
+          const unsigned s = scale_byte(block_magnitude(x, quad_magnitude));
+          const float scale = scale_value(s);
+          codes.store8<kNonTemporal>(at(step), to_codes(x[0], x[1], x[2], x[3], scale), to_codes(x[4], x[5], x[6], x[7], scale));
+          scales_of.store1(lane & 3 ? kNowhere : scale_at(step), s);
+        };
+        if (a.far) y.store16<kNonTemporal>(2 * at(step), words(v));
+        else y.store16(2 * at(step), words(v));
+        if (!kGrad && a.z) {
+          if (a.z_scales) store_8bit(z_out, z_scale, z);
+          else z_out.store16<kNonTemporal>(2 * at(step), words(z));
+        }
+        if (!kGrad && a.y_codes) store_8bit(y_code, y_scale, v);
+      }
+    }
+  }
+}
+template <int kFA, int kNB, int kArea, bool kGrad>
+__device__ __forceinline__ void finish(const LinearStart& p, const LinearArgs& a, const f32x4 (&sum)[kFA][kNB], char* area, int t_first, int f_first) {
+  if (f_first >= p.O || t_first >= p.T) return;   // (the whole wavefront)
+  auto as = [&](auto z, auto kind) {
+    constexpr int kZ = decltype(z)::value, kAct = decltype(kind)::value;
+    if (a.add) finish_as<kFA, kNB, kArea, kGrad, kZ, true, kAct>(p, a, sum, area, t_first, f_first);
+    else finish_as<kFA, kNB, kArea, kGrad, kZ, false, kAct>(p, a, sum, area, t_first, f_first);
+  };
+  typedef std::integral_constant<int, kZNone> NoZ;
+  if constexpr (kGrad) {
+    if (a.act == kActNone) as(NoZ(), std::integral_constant<int, kActNone>());
+    else with_activation(a.act, [&](auto kind) {
+      if constexpr (decltype(kind)::value != kActNone) {
+        if (a.z_in_scales) as(std::integral_constant<int, kZCodes>(), kind);
+        else as(std::integral_constant<int, kZBf16>(), kind);
+      }
+    });
+  } else {
+    with_activation(a.act, [&](auto kind) { as(NoZ(), kind); });
+  }
+}
+
+// One group, two stages of 64 terms: a wavefront reads a slice of 32 terms from LDS while it multiplies the slice before, also across
+// the one barrier of a stage, which stands between its two slices: there everyone has read the second one, so that the stage's space can be
+// filled again, and the next stage, issued a stage ago, has landed.  Reads and loads are dealt among the products one by one: the
+// eight wavefronts' loads of a stage take the address unit half of its products' time, and issued together they keep everyone from multiplying.
+// `prepare(s)` is called before the loads of stage s, `load(s, i)` issues one of them (stages 0 and 1 are under way), `landed(s)` is
+// called when all of this wavefront's have landed, before others see them; `per_slice` gets operand B of each slice.
+template <class S, bool kTA, bool kTB, class Prepare, class Load, class Landed, class PerSlice>
+__device__ __forceinline__ void contract_pipelined(const char* ring, int nk, const FragOffsets& fa, const FragOffsets& fb, int wa, int wb,
+                                                   f32x4 (&acc)[S::kFA][S::kFB], Prepare&& prepare, Load&& load, Landed&& landed,
+                                                   PerSlice&& per_slice) {
+  bf16x8 a[2][S::kFA], b[2][S::kFB];
+  auto read_a = [&](const char* stage, int k, int i) {
+    a[k][i] = read_frag<kTA>(stage + (kTA ? 0 : wa * S::kFA * 16 * 128), fa, (kTA ? wa * S::kFA : 0) + i, k);
+  };
+  auto read_b = [&](const char* stage, int k, int j) {
+    b[k][j] = read_frag<kTB>(stage + S::kA * kTileBytes + (kTB ? 0 : wb * S::kFB * 16 * 128), fb, (kTB ? wb * S::kFB : 0) + j, k);
+  };
+  // Multiplies slice k; reads slice 1 - k of `stage`; and issues the loads of stage s.
+  auto part = [&](auto slice, const char* stage, int s) {
+    constexpr int k = decltype(slice)::value, kEach = (S::kLoads + S::kFA - 1) / S::kFA;
+#pragma unroll
+    for (int i = 0; i < S::kFA; ++i) {
+      if (k == 1 && s < nk)
+#pragma unroll
+        for (int l = i * kEach; l < min((i + 1) * kEach, S::kLoads); ++l) load(s, l);
+#pragma unroll
+      for (int j = i * S::kFB / S::kFA; j < (i + 1) * S::kFB / S::kFA; ++j) read_b(stage, 1 - k, j);
+      read_a(stage, 1 - k, i);
+#pragma unroll
+      for (int j = 0; j < S::kFB; ++j) acc[i][j] = mfma16(a[k][i], b[k][j], acc[i][j]);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    per_slice(b[k]);
+  };
+  // lgkmcnt(0), in the form that the compiler takes account of: with asm it waits for the next slice's reads before the first product
+  constexpr int kReadsDone = 0xc07f;
+  wait_vmcnt_le<S::kLoads>(nk > 1 ? S::kLoads : 0);
+  landed(0);
+  barrier_no_fence();
+#pragma unroll
+  for (int j = 0; j < S::kFB; ++j) read_b(ring, 0, j);
+#pragma unroll
+  for (int i = 0; i < S::kFA; ++i) read_a(ring, 0, i);
+  __builtin_amdgcn_s_waitcnt(kReadsDone);
+  for (int s = 0; s < nk; ++s) {
+    const char *now = ring + (s & 1) * S::kStageBytes, *next = ring + (~s & 1) * S::kStageBytes;
+    __builtin_amdgcn_sched_barrier(0);
+    part(std::integral_constant<int, 0>(), now, 0);
+    __builtin_amdgcn_s_waitcnt(kReadsDone);
+    if (s + 1 < nk) {
+      wait_vmcnt_le<0>(0);
+      landed(s + 1);
+    }
+    barrier_no_fence();
+    __builtin_amdgcn_sched_barrier(0);
+    if (s + 2 < nk) prepare(s + 2);
+    part(std::integral_constant<int, 1>(), next, s + 2);   // (behind the last stage it reads whatever is there, for nothing)
+    __builtin_amdgcn_s_waitcnt(kReadsDone);
+  }
 }
 
 template <class S, bool kGrad>
@@ -59,7 +291,6 @@ __device__ __forceinline__ void linear_tile(const LinearStart& p, const LinearAr
   const int wave_id = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int group = wave_id / S::kWaves, wave = wave_id - group * S::kWaves;
   const int wa = wave / S::kWB, wb = wave - wa * S::kWB;
-  const int r = lane & 15, quarter = lane >> 4;
   char* const ring = lds + group * S::kRingBytes;
   const int rows = min(S::kRowsB, p.T - t0), feats = min(S::kRowsA, p.O - f0);
 
@@ -83,31 +314,35 @@ __device__ __forceinline__ void linear_tile(const LinearStart& p, const LinearAr
   const int stages = (p.K + 63) >> 6, nk = (stages + S::kGroups - 1) / S::kGroups;   // nk: this group's, the last one short or empty
   const int short_k = 64 * ((nk - 1) * S::kGroups + group);   // its first term
   const bool is_short = short_k + 64 > p.K;
-  auto issue_stage = [&](int g) {
-    char* st = ring + (g % S::kStages) * S::kStageBytes;
+  // Before a stage's loads: the short one's repeat the last 16 bytes, or rows (no other stage follows).
+  auto prepare_stage = [&](int g) {
     if (__builtin_expect(g == nk - 1 && is_short, 0)) {
       const int row0 = min(short_k, p.K - 1);
-      const char *w_base = uniform_ptr(kGrad ? w0 + (size_t)row0 * p.O * 2 : w0), *x_base = uniform_ptr(x0);
+      w_ptr = kGrad ? w0 + (size_t)row0 * p.O * 2 : w0;
+      x_ptr = x0;
 #pragma unroll
       for (int i = 0; i < S::kLoads; ++i) {
         const bool is_a = i < S::kLoadsA;
-        const int y = is_a ? i : i - S::kLoadsA;
-        const LoadUnit l = load_unit<S::kWaves>(wave, lane, y);
-        unsigned o = off[i];
-        if (kGrad && is_a) o -= (unsigned)(l.row - (min(short_k + l.row, p.K - 1) - row0)) * (unsigned)p.O * 2;
-        else o += (unsigned)min(short_k + 8 * l.chunk, p.K - 8) * 2 - l.chunk * 16;
-        load_to_lds_16(is_a ? w_base : x_base, o, st + (is_a ? 0 : S::kA * kTileBytes) + load_dst<S::kWaves>(wave, y));
+        const LoadUnit l = load_unit<S::kWaves>(wave, lane, is_a ? i : i - S::kLoadsA);
+        if (kGrad && is_a) off[i] -= (unsigned)(l.row - (min(short_k + l.row, p.K - 1) - row0)) * (unsigned)p.O * 2;
+        else off[i] += (unsigned)min(short_k + 8 * l.chunk, p.K - 8) * 2 - l.chunk * 16;
       }
-      return;
     }
-    const char *w_base = uniform_ptr(w_ptr), *x_base = uniform_ptr(x_ptr);
+  };
+  auto load_one = [&](int g, int i) {
+    char* st = ring + (g % S::kStages) * S::kStageBytes;
+    const bool is_a = i < S::kLoadsA;
+    load_to_lds_16(uniform_ptr(is_a ? w_ptr : x_ptr), off[i],
+                   st + (is_a ? 0 : S::kA * kTileBytes) + load_dst<S::kWaves>(wave, is_a ? i : i - S::kLoadsA));
+    if (i == S::kLoads - 1) {
+      w_ptr += S::kGroups * w_step;
+      x_ptr += S::kGroups * 128;
+    }
+  };
+  auto issue_stage = [&](int g) {
+    prepare_stage(g);
 #pragma unroll
-    for (int i = 0; i < S::kLoadsA; ++i) load_to_lds_16(w_base, off[i], st + load_dst<S::kWaves>(wave, i));
-#pragma unroll
-    for (int i = 0; i < S::kLoadsB; ++i)
-      load_to_lds_16(x_base, off[S::kLoadsA + i], st + S::kA * kTileBytes + load_dst<S::kWaves>(wave, i));
-    w_ptr += S::kGroups * w_step;
-    x_ptr += S::kGroups * 128;
+    for (int i = 0; i < S::kLoads; ++i) load_one(g, i);
   };
   // My share of the short stage, landed, is zero from the last term on.
   auto clear_short = [&]() {
@@ -122,31 +357,17 @@ __device__ __forceinline__ void linear_tile(const LinearStart& p, const LinearAr
     }
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
   };
-  constexpr bool kHalves = S::kGroups == 1 && S::kWaves == 8 && S::kStages == 2;
+  constexpr bool kPipelined = S::kGroups == 1 && S::kStages == 2;
 #pragma unroll
-  for (int s = 0; s < S::kStages - 1; ++s)
+  for (int s = 0; s < (kPipelined ? S::kStages : S::kStages - 1); ++s)
     if (s < nk) issue_stage(s);
 
-  // While the first stages travel: which tokens are padding, and the bias of this lane's features.
-  const unsigned char* const fl = a.flags ? a.flags + t0 : nullptr;
-  bool any = !fl;
-  const int j0 = wb * S::kFB + group * S::kOutB;  // first block of tokens that this wavefront stores
-  int row[S::kOutB];
-  unsigned pad_bits = 0;
+  // While the first stages travel: is any token of the tile not padding (every wavefront looks at all of them)?
+  bool any = !a.flags;
+  if (a.flags) {
 #pragma unroll
-  for (int j = 0; j < S::kOutB; ++j) row[j] = min((j0 + j) * 16 + r, rows - 1);
-  if (fl) {
-#pragma unroll
-    for (int i = 0; i < S::kB; ++i) any |= fl[min(64 * i + lane, rows - 1)] < 2;
-#pragma unroll
-    for (int j = 0; j < S::kOutB; ++j) pad_bits |= (unsigned)(fl[row[j]] >= 2) << j;
+    for (int i = 0; i < S::kB; ++i) any |= a.flags[t0 + min(64 * i + lane, rows - 1)] < 2;
   }
-  f32x4 bias[S::kFA];
-#pragma unroll
-  for (int i = 0; i < S::kFA; ++i) bias[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-  if (!kGrad && a.bias)
-#pragma unroll
-    for (int i = 0; i < S::kFA; ++i) bias[i] = *reinterpret_cast<const f32x4*>(a.bias + f0 + min((wa * S::kFA + i) * 16 + 4 * quarter, feats - 4));
 
   f32x4 acc[S::kFA][S::kFB];
 #pragma unroll
@@ -157,133 +378,32 @@ __device__ __forceinline__ void linear_tile(const LinearStart& p, const LinearAr
     FragOffsets fa, fb;
     frag_offsets<kGrad>(fa, lane);
     frag_offsets<false>(fb, lane);
-    // the second half, or group, follows one barrier behind
-    const bool apart = kHalves || S::kAlternate, second = kHalves ? wave >= 4 : group == 1;
-    if (kHalves) {
-      wait_vmcnt_le<0>(0);
-      if (is_short && nk == 1) clear_short();
-    }
+    if constexpr (kPipelined) {
+      contract_pipelined<S, kGrad, false>(ring, nk, fa, fb, wa, wb, acc, prepare_stage, load_one,
+                                          [&](int s) { if (__builtin_expect(is_short && s == nk - 1, 0)) clear_short(); },
+                                          [](const bf16x8 (&)[S::kFB]) {});
+    } else {
+    // the second group follows one barrier behind
+    const bool apart = S::kAlternate, second = group == 1;
     if (apart && second) barrier_no_fence();
     for (int ks = 0; ks < nk; ++ks) {
       // stage ks has landed: everything but the younger stages' loads (fewer near the end)
-      if (!kHalves) {
-        wait_vmcnt_le<S::kLoads * (S::kStages - 2)>(min(S::kStages - 2, nk - 1 - ks) * S::kLoads);
-        if (__builtin_expect(is_short && ks == nk - 1, 0)) clear_short();
-      }
+      wait_vmcnt_le<S::kLoads * (S::kStages - 2)>(min(S::kStages - 2, nk - 1 - ks) * S::kLoads);
+      if (__builtin_expect(is_short && ks == nk - 1, 0)) clear_short();
       barrier_no_fence();  // ... for every wavefront, and everyone is done with stage ks - 1
-      contract_stage<S, kGrad, false, kHalves>(ring + (ks % S::kStages) * S::kStageBytes, fa, fb, wa, wb, acc,
-                                               [&]() { if (ks + S::kStages - 1 < nk) issue_stage(ks + S::kStages - 1); },
-                                               [](const bf16x8 (&)[S::kFB]) {},
-                                               [&]() {
-                                                 wait_vmcnt_le<0>(0);
-                                                 if (__builtin_expect(is_short && ks == nk - 2, 0)) clear_short();
-                                               },
-                                               []() {});
+      contract_stage<S, kGrad, false, false>(ring + (ks % S::kStages) * S::kStageBytes, fa, fb, wa, wb, acc,
+                                             [&]() { if (ks + S::kStages - 1 < nk) issue_stage(ks + S::kStages - 1); },
+                                             [](const bf16x8 (&)[S::kFB]) {}, []() {}, []() {});
     }
     if (apart && !second) barrier_no_fence();
+    }
   }
   f32x4 sum[S::kFA][S::kOutB];
   add_groups<S>(acc, sum, lds, group, wave, lane);
 
-  // ---- epilogue, in fp32 until a result is rounded.  A lane holds features 16 i + 4 quarter .. + 3 of token 16 j + r; memory is read
-  // and written in eight consecutive ones, 64 of a token's bytes per instruction (32 of codes).  A pair of blocks is a block of one
-  // scale, its 32 values in the four quarters. ----
-  const int scales = scale_blocks(p.O);
-  const int lane_feature = (quarter & 1) * 16 + (quarter >> 1) * 8;   // first of the eight, in the pair
-  auto magnitude_across = [](unsigned m) {
-    const Pair x = exchange(m, m);
-    m = max(x.u[0], x.u[1]);
-    const auto y = __builtin_amdgcn_permlane32_swap(m, m, false, false);
-    return max((unsigned)y[0], (unsigned)y[1]);
-  };
-  with_activation(a.act, [&](auto kind) {
-    constexpr int kAct = decltype(kind)::value;
-#pragma unroll
-    for (int i = 0; i < S::kFA; i += 2) {
-      const int fw = (wa * S::kFA + i) * 16;       // first feature of the pair in the tile
-      if (fw >= feats) break;
-      const bool stored = fw + lane_feature < feats;
-      const bool real[2] = {fw + 4 * quarter < feats, fw + 16 + 4 * quarter < feats};   // this lane's four features of each block
-      const size_t at0 = (size_t)t0 * p.O + f0 + fw + lane_feature, scale0 = (size_t)t0 * scales + (f0 + fw) / kScaleBlock;
-      u32x4 add[S::kOutB], zb[S::kOutB];
-      unsigned zs[S::kOutB];
-#pragma unroll
-      for (int j = 0; j < S::kOutB; ++j) {
-        const size_t at = at0 + (size_t)row[j] * p.O;
-        add[j] = zb[j] = u32x4{0, 0, 0, 0};
-        zs[j] = 1;
-        if (stored && a.add) add[j] = *reinterpret_cast<const u32x4*>(a.add + at);
-        if (kGrad && kAct != kActNone) {
-          if (a.z_in_scales) {
-            zs[j] = a.z_in_scales[scale0 + (size_t)row[j] * scales];
-            if (stored) {
-              const uint2 w = *reinterpret_cast<const uint2*>(static_cast<const unsigned char*>(a.z_in) + at);
-              zb[j][0] = w.x;
-              zb[j][1] = w.y;
-            }
-          } else if (stored) {
-            zb[j] = *reinterpret_cast<const u32x4*>(static_cast<const unsigned short*>(a.z_in) + at);
-          }
-        }
-      }
-#pragma unroll
-      for (int j = 0; j < S::kOutB; ++j) {
-        const bool pad = (pad_bits >> j) & 1u, store = stored && (j0 + j) * 16 + r < rows;
-        const size_t at = at0 + (size_t)row[j] * p.O, scale_at = scale0 + (size_t)row[j] * scales;
-        const Pair add_lo = exchange(add[j][0], add[j][2]), add_hi = exchange(add[j][1], add[j][3]);
-        float v[8], z[8];
-        if (kGrad && kAct != kActNone) {
-          if (a.z_in_scales) {
-            const Pair c = exchange(zb[j][0], zb[j][1]);
-            const f32x4 lo = from_codes(c.u[0], scale_value(zs[j])), hi = from_codes(c.u[1], scale_value(zs[j]));
-#pragma unroll
-            for (int e = 0; e < 4; ++e) { z[e] = lo[e]; z[4 + e] = hi[e]; }
-          } else {
-            const Pair lo = exchange(zb[j][0], zb[j][2]), hi = exchange(zb[j][1], zb[j][3]);
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-              z[4 * h] = low_bf16(lo.u[h]); z[4 * h + 1] = high_bf16(lo.u[h]);
-              z[4 * h + 2] = low_bf16(hi.u[h]); z[4 * h + 3] = high_bf16(hi.u[h]);
-            }
-          }
-        }
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const f32x4 c = sum[i + h][j] + bias[i + h];
-          const float more[4] = {low_bf16(add_lo.u[h]), high_bf16(add_lo.u[h]), low_bf16(add_hi.u[h]), high_bf16(add_hi.u[h])};
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            float x;
-            if constexpr (kGrad) {
-              x = kAct == kActNone ? c[e] : c[e] * slope<kAct>(z[4 * h + e]);
-            } else {
-              z[4 * h + e] = pad || !real[h] ? 0.f : c[e];
-              x = activate<kAct>(c[e]);
-            }
-            if (a.add) x += more[e];
-            v[4 * h + e] = pad || !real[h] ? 0.f : x;
-          }
-        }
-        auto store_bf16 = [&](unsigned short* to, const float (&x)[8]) {
-          const Pair lo = exchange(pack2(x[0], x[1]), pack2(x[4], x[5])), hi = exchange(pack2(x[2], x[3]), pack2(x[6], x[7]));
-          if (store) *reinterpret_cast<u32x4*>(to + at) = u32x4{lo.u[0], hi.u[0], lo.u[1], hi.u[1]};
-        };
-        auto store_8bit = [&](unsigned char* to, unsigned char* to_scales, float (&x)[8]) {
-          const unsigned s = scale_byte(block_magnitude(x, magnitude_across));
-          const float scale = scale_value(s);
-          const Pair c = exchange(to_codes(x[0], x[1], x[2], x[3], scale), to_codes(x[4], x[5], x[6], x[7], scale));
-          if (store) *reinterpret_cast<uint2*>(to + at) = make_uint2(c.u[0], c.u[1]);
-          if (store && quarter == 0) to_scales[scale_at] = (unsigned char)s;
-        };
-        if (!kGrad && a.z) {
-          if (a.z_scales) store_8bit(static_cast<unsigned char*>(a.z), a.z_scales, z);
-          else store_bf16(static_cast<unsigned short*>(a.z), z);
-        }
-        store_bf16(a.y, v);
-        if (!kGrad && a.y_codes) store_8bit(a.y_codes, a.y_scales, v);
-      }
-    }
-  });
+  constexpr int kWaveArea = S::kLds / S::kAllWaves, kArea = std::min(S::kOutB, kWaveArea / (S::kFA * 1024));
+  __syncthreads();   // (everyone is done with the stages)
+  finish<S::kFA, S::kOutB, kArea, kGrad>(p, a, sum, lds + wave_id * kWaveArea, t0 + (wb * S::kFB + group * S::kOutB) * 16, f0 + wa * S::kFA * 16);
 }
 
 template <class S, bool kGrad>
@@ -319,6 +439,7 @@ hipError_t launch_product(LinearArgs a, hipStream_t stream) {
     range_rows = (int)(std::max<size_t>(1, std::min<size_t>(1024 * 256 / S::kThreads, a.ranges.n / 4 / S::kThreads)) + x - 1) / x;
     a.ranges.blocks = range_rows * x;
   }
+  a.far = (size_t)a.T * a.O * 2 > (96u << 20);
   const int y = d.grid_y() + range_rows;
   const dim3 grid(x, std::min(y, kMostGridY), (y + kMostGridY - 1) / kMostGridY);
   const hipError_t e = allow_lds<&linear_kernel<S, kGrad>>(S::kLds);
@@ -354,6 +475,121 @@ hipError_t run_product(const LinearArgs& a, hipStream_t stream) {
   offer(Tile64(), 0.46, 0.74, 0.53);
   offer(Tile64x2(), 0.39, 0.8, 0.71);
   return launch(a, stream);
+}
+
+// ---- few tokens ------------------------------------------------------------------------------------
+// Up to 64 tokens: what takes time is reading the weights, and latency.  A workgroup has kRows features and all tokens; its wavefronts
+// share the contraction and read operands straight from memory into registers (a lane holds 16 of 64 terms, so that a row's 128
+// bytes are read together; both operands hold the same ones).  Their sums are added through LDS, in the order of the wavefronts.
+// A compute unit has only so many reads under way, so that all of them should share the weights: where 16 features a workgroup
+// leave units without one, a workgroup has 8 or 4, and the 16 rows of an operand are those at 2 or 4 places of the contraction, each
+// multiplied with the tokens at all of these places, of which one product in 2 or 4 counts (there is time for that).
+template <int kRows, int kFB, int kWaves>
+__global__ __launch_bounds__(64 * kWaves) void few_kernel(const unsigned short* w, const unsigned short* tok, int T, int O, int K, LinearArgs a) {
+  constexpr int kParts = 16 / kRows, kDepth = std::max(1, 4 / kParts / (kFB > 2 ? 2 : 1));   // kDepth: steps whose loads travel together
+  __shared__ f32x4 part[kWaves][kFB][64];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, q = lane >> 4;
+  const int f0 = blockIdx.x * kRows;
+  const unsigned short *row_w = w + (size_t)min(f0 + r % kRows, O - 1) * K + 64 * (r / kRows) + 8 * q, *rows_x[kFB];
+  const int first = 64 * (r / kRows) + 8 * q;   // of this lane's terms of the weights in a step
+#pragma unroll
+  for (int j = 0; j < kFB; ++j) rows_x[j] = tok + (size_t)min(16 * j + r, T - 1) * K + 8 * q;
+  f32x4 acc[kParts][kFB];
+#pragma unroll
+  for (int s = 0; s < kParts; ++s)
+#pragma unroll
+    for (int j = 0; j < kFB; ++j) acc[s][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  bf16x8 fw[kDepth][2], fx[kDepth][kParts][kFB][2];
+  auto multiply = [&](int d) {
+#pragma unroll
+    for (int s = 0; s < kParts; ++s)
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int j = 0; j < kFB; ++j) acc[s][j] = mfma16_apart(fw[d][h], fx[d][s][j][h], acc[s][j]);
+  };
+  constexpr int kTerms = 64 * kParts;   // of a step
+  auto load = [&](int d, int c, auto&& one) {   // one(address, first term)
+    const int at = c * kTerms;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      fw[d][h] = one(row_w + at + 32 * h, at + first + 32 * h);
+#pragma unroll
+      for (int s = 0; s < kParts; ++s)
+#pragma unroll
+        for (int j = 0; j < kFB; ++j) fx[d][s][j][h] = one(rows_x[j] + at + 64 * s + 32 * h, at + 64 * s + 8 * q + 32 * h);
+    }
+  };
+  const int steps = (K + kTerms - 1) / kTerms, each = (steps + kWaves - 1) / kWaves, end = min(steps, (wave + 1) * each), whole = min(end, K / kTerms);
+  int c = wave * each;
+  for (; c + kDepth <= whole; c += kDepth) {
+#pragma unroll
+    for (int d = 0; d < kDepth; ++d) load(d, c + d, [](const unsigned short* p, int) { return *reinterpret_cast<const bf16x8*>(p); });
+#pragma unroll
+    for (int d = 0; d < kDepth; ++d) multiply(d);
+  }
+  for (; c < end; c += kDepth) {   // the last ones: what is past the end is zero
+    const int stop = min(K, end * kTerms);
+#pragma unroll
+    for (int d = 0; d < kDepth; ++d)
+      load(d, c + d, [&](const unsigned short* p, int k) { return k < stop ? *reinterpret_cast<const bf16x8*>(p) : bf16x8{}; });
+#pragma unroll
+    for (int d = 0; d < kDepth; ++d) multiply(d);
+  }
+  // Rows 4 q .. + 3 of a product: kRows = 4: features 0 .. 3 at place q; 8: features 4 (q % 2) .. + 3 at place q / 2.
+#pragma unroll
+  for (int j = 0; j < kFB; ++j) {
+    f32x4 x = acc[0][j];
+#pragma unroll
+    for (int s = 1; s < kParts; ++s)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[e] = q * kParts / 4 == s ? acc[s][j][e] : x[e];
+    part[wave][j][lane] = x;
+  }
+  __syncthreads();
+  if (wave >= kFB) return;
+  f32x4 z = part[0][wave][lane];
+#pragma unroll
+  for (int v = 1; v < kWaves; ++v) z += part[v][wave][lane];
+  if (kParts > 1)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) z[e] = kParts == 4 ? quad_sum(z[e]) : half_sum(z[e]);
+  const int t = 16 * wave + r, f = f0 + 4 * q;   // a lane's four features of a token
+  if (t >= T || f >= O || 4 * q >= kRows) return;
+  const size_t at = (size_t)t * O + f;
+  uint2 add = make_uint2(0, 0);
+  if (a.add) add = *reinterpret_cast<const uint2*>(a.add + at);
+  if (a.bias) z += *reinterpret_cast<const f32x4*>(a.bias + f);
+  const bool pad = a.flags && a.flags[t] >= 2;
+  f32x4 y = z;
+  with_activation(a.act, [&](auto kind) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) y[e] = activate<decltype(kind)::value>(z[e]);
+  });
+  if (a.add) y += f32x4{low_bf16(add.x), high_bf16(add.x), low_bf16(add.y), high_bf16(add.y)};
+  if (pad) y = z = f32x4{0.f, 0.f, 0.f, 0.f};
+  if (a.z) *reinterpret_cast<uint2*>(static_cast<unsigned short*>(a.z) + at) = make_uint2(pack2(z[0], z[1]), pack2(z[2], z[3]));
+  *reinterpret_cast<uint2*>(a.y + at) = make_uint2(pack2(y[0], y[1]), pack2(y[2], y[3]));
+}
+template <int kRows, int kFB>
+hipError_t launch_few(const LinearArgs& a, hipStream_t stream) {
+  constexpr int kWaves = 8;
+  hipLaunchKernelGGL((few_kernel<kRows, kFB, kWaves>), dim3((a.O + kRows - 1) / kRows), dim3(64 * kWaves), 0, stream, a.w, a.tok, a.T, a.O, a.K, a);
+  return hipGetLastError();
+}
+template <int kRows>
+hipError_t launch_few(const LinearArgs& a, hipStream_t stream) {
+  if constexpr (kRows > 4)
+    if (a.T > 32) return launch_few<kRows, 4>(a, stream);
+  return a.T <= 16 ? launch_few<kRows, 1>(a, stream) : launch_few<kRows, 2>(a, stream);
+}
+// us (in a graph, weights not in the L2), 16, 8 and 4 features a workgroup: 4096 -> 1024 at 1 token 6.6, 5.4, 4.5, at 16 9.2, 7.7, 7.3, at 32 12.6, 11.2, 11.0;
+// 2048 -> 768 at 1 4.4, 3.6, 3.4; 1024 -> 1024 at 16 3.9, 3.7, 3.8; 1024 -> 4096 at 1 3.9, 4.3, 4.7, at 24 5.2, 6.7, 10.7 (and 8.6 as a product of tiles),
+// at 64 7.0, 10.8, 23.5 (8.9).
+constexpr int kFewTokens = 64;
+hipError_t run_few(const LinearArgs& a, hipStream_t stream) {
+  if (a.O > 2048) return launch_few<16>(a, stream);
+  return a.O > 1024 || a.T > 32 ? launch_few<8>(a, stream) : launch_few<4>(a, stream);
 }
 
 // ======================================================================================
@@ -432,20 +668,26 @@ __global__ __launch_bounds__(S::kThreads, S::kAllWaves / 4 * S::kPerCU) void lin
     off[i] = (unsigned)l.row * (is_x ? x_stride : g_stride) + (unsigned)min((is_x ? e0 : f0) + 64 * l.tile + 8 * l.chunk, (is_x ? a.E : a.F) - 8) * 2;
   }
   const int last_block = total_blocks - 1, last_rows = a.T - 64 * last_block;
-  auto issue_stage = [&](int block, int slot) {
-    char* st = ring + slot * S::kStageBytes;
+  const char *x_base = nullptr, *g_base = nullptr;   // of the stage being loaded
+  bool at_end = false;
+  auto prepare_block = [&](int block) {
     block = __builtin_amdgcn_readfirstlane(block);
-    const char* const x_base = uniform_ptr(reinterpret_cast<const char*>(a.x) + (size_t)block * 64 * x_stride);
-    const char* const g_base = uniform_ptr(reinterpret_cast<const char*>(a.g) + (size_t)block * 64 * g_stride);
+    x_base = uniform_ptr(reinterpret_cast<const char*>(a.x) + (size_t)block * 64 * x_stride);
+    g_base = uniform_ptr(reinterpret_cast<const char*>(a.g) + (size_t)block * 64 * g_stride);
+    at_end = block == last_block;
+  };
+  auto load_one = [&](int slot, int i) {
+    const bool is_x = i < S::kLoadsA;
+    const int y = is_x ? i : i - S::kLoadsA;
+    unsigned o = off[i];
+    if (__builtin_expect(at_end, 0))   // rows past the end repeat the last one, and are cleared like pad rows
+      o -= (unsigned)max(0, load_unit<S::kWaves>(wave, lane, y).row - (last_rows - 1)) * (is_x ? x_stride : g_stride);
+    load_to_lds_16(is_x ? x_base : g_base, o, ring + slot * S::kStageBytes + (is_x ? 0 : S::kA * kTileBytes) + load_dst<S::kWaves>(wave, y));
+  };
+  auto issue_stage = [&](int block, int slot) {
+    prepare_block(block);
 #pragma unroll
-    for (int i = 0; i < S::kLoads; ++i) {
-      const bool is_x = i < S::kLoadsA;
-      const int y = is_x ? i : i - S::kLoadsA;
-      unsigned o = off[i];
-      if (block == last_block)   // rows past the end repeat the last one, and are cleared like pad rows
-        o -= (unsigned)max(0, load_unit<S::kWaves>(wave, lane, y).row - (last_rows - 1)) * (is_x ? x_stride : g_stride);
-      load_to_lds_16(is_x ? x_base : g_base, o, st + (is_x ? 0 : S::kA * kTileBytes) + load_dst<S::kWaves>(wave, y));
-    }
+    for (int i = 0; i < S::kLoads; ++i) load_one(slot, i);
   };
 
   f32x4 acc[S::kFA][S::kFB];
@@ -460,11 +702,12 @@ __global__ __launch_bounds__(S::kThreads, S::kAllWaves / 4 * S::kPerCU) void lin
   FragOffsets fo;
   frag_offsets<true>(fo, lane);
 
+  constexpr bool kPipelined = S::kGroups == 1 && S::kStages == 2;
 #pragma unroll
-  for (int k = 0; k + 1 < S::kStages; ++k)
+  for (int k = 0; k + (kPipelined ? 0 : 1) < S::kStages; ++k)
     if (i_begin + group + k * S::kGroups < i_end) issue_stage(live_block[i_begin + group + k * S::kGroups], k);
   auto land = [&](int i, int it) {
-    wait_vmcnt_le<S::kLoads * (S::kStages - 2)>(max(0, min(S::kStages - 2, (i_end - 1 - i) / S::kGroups)) * S::kLoads);
+    if (!kPipelined) wait_vmcnt_le<S::kLoads * (S::kStages - 2)>(max(0, min(S::kStages - 2, (i_end - 1 - i) / S::kGroups)) * S::kLoads);
     const unsigned long long padmask = S::kGroups == 1 || i < i_end ? live_mask[i] : ~0ull;   // (an odd last block leaves group 1 padding only)
     if (padmask) {
       char* st = ring + (it % S::kStages) * S::kStageBytes;
@@ -478,23 +721,29 @@ __global__ __launch_bounds__(S::kThreads, S::kAllWaves / 4 * S::kPerCU) void lin
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     }
   };
-  if (S::kAlternate && group == 1) barrier_no_fence();  // group 1 follows one barrier behind
-  for (int i0 = i_begin, it = 0; i0 < i_end; i0 += S::kGroups, ++it) {
-    const int i = i0 + group, ahead = i + (S::kStages - 1) * S::kGroups;
-    const int next = live_block[min(ahead, i_end - 1)];
-    land(i, it);
-    barrier_no_fence();          // landed for everyone; and everyone is done with the block before it
-    contract_stage<S, true, true, false>(ring + (it % S::kStages) * S::kStageBytes, fo, fo, wa, wb, acc,
-                                         [&]() { if (ahead < i_end) issue_stage(next, (it + S::kStages - 1) % S::kStages); },
-                                         [&](const bf16x8 (&g)[S::kFB]) {
-                                           if (do_bias) {
+  auto add_bias = [&](const bf16x8 (&g)[S::kFB]) {
+    if (do_bias) {
 #pragma unroll
-                                             for (int j = 0; j < S::kFB; ++j) bias_acc[j] = sum8(g[j], bias_acc[j]);
-                                           }
-                                         },
-                                         []() {}, []() {});
+      for (int j = 0; j < S::kFB; ++j) bias_acc[j] = sum8(g[j], bias_acc[j]);
+    }
+  };
+  if constexpr (kPipelined) {
+    if (i_begin < i_end)
+      contract_pipelined<S, true, true>(ring, i_end - i_begin, fo, fo, wa, wb, acc, [&](int s) { prepare_block(live_block[i_begin + s]); },
+                                        [&](int s, int i) { load_one(s & 1, i); }, [&](int s) { land(i_begin + s, s); }, add_bias);
+  } else {
+    if (S::kAlternate && group == 1) barrier_no_fence();  // group 1 follows one barrier behind
+    for (int i0 = i_begin, it = 0; i0 < i_end; i0 += S::kGroups, ++it) {
+      const int i = i0 + group, ahead = i + (S::kStages - 1) * S::kGroups;
+      const int next = live_block[min(ahead, i_end - 1)];
+      land(i, it);
+      barrier_no_fence();          // landed for everyone; and everyone is done with the block before it
+      contract_stage<S, true, true, false>(ring + (it % S::kStages) * S::kStageBytes, fo, fo, wa, wb, acc,
+                                           [&]() { if (ahead < i_end) issue_stage(next, (it + S::kStages - 1) % S::kStages); }, add_bias,
+                                           []() {}, []() {});
+    }
+    if (S::kAlternate && group == 0) barrier_no_fence();
   }
-  if (S::kAlternate && group == 0) barrier_no_fence();
   f32x4 sum[S::kFA][S::kOutB];
   add_groups<S>(acc, sum, lds, group, wave, lane);
 
@@ -593,6 +842,7 @@ hipError_t launch_linear(const LinearCall& c, hipStream_t stream) {
   a.z_scales = c.z_scales;
   a.y_codes = c.y_codes;
   a.y_scales = c.y_scales;
+  if (a.T <= kFewTokens && !a.z_scales && !a.y_codes) return run_few(a, stream);
   return run_product<false>(a, stream);
 }
 
