@@ -378,7 +378,8 @@ mate_status mate_out_project_bwd(const void* o, const void* w_o, const uint8_t* 
  *             no activation (act is MATE_ACT_NONE then, and z NULL)
  *   residual  gradient that reached x on another way, [B, N, E] bf16, or NULL; may be dx itself
  *   dx, dw, dbias   any may be NULL (not computed); dbias needs dw
- *   workspace mate_linear_bwd_workspace_bytes(B, N, E, F, x_scales != NULL) bytes (0: sizes out of range); needed for dw only
+ *   workspace mate_linear_bwd_workspace_bytes(B, N, E, F, x_scales != NULL) bytes (0: sizes out of range), at any address;
+ *             needed for dw only
  * A layer y = act(x w^T + b) whose next product is y w2^T: mate_linear_bwd of the second with z and act of the first gives the
  * gradient at z, which is dy of the first one's mate_linear_bwd.  The result does not depend on whether the other gradient is wanted.
  *

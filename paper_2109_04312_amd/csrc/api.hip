@@ -346,7 +346,7 @@ mate_status mate_linear_bwd(const void* dy, const void* x, const uint8_t* x_scal
       !aligned({dy, x, w, z, residual, dx, dw, dbias}))
     return MATE_ERR_UNSUPPORTED;
   if (dw && (!workspace || workspace_bytes < linear_bwd_workspace(B * N, E, F, x_scales != nullptr))) return MATE_ERR_WORKSPACE;
-  const LinearBwdCall c = {dy, x, x_scales, w, flags, z, z_scales, residual, B * N, E, F, act, dx, dw, dbias, workspace};
+  const LinearBwdCall c = {dy, x, x_scales, w, flags, z, z_scales, residual, B * N, E, F, act, dx, dw, dbias, workspace, next_ticket()};
   return done(launch_linear_bwd(c, static_cast<hipStream_t>(stream)));
 }
 

@@ -148,6 +148,7 @@ struct LinearBwdCall {
   void* dx;
   float *dw, *dbias;
   void* workspace;
+  unsigned long long ticket;   // see arrival.h
 };
 size_t linear_bwd_workspace(int T, int E, int F, bool codes);
 hipError_t launch_linear_bwd(const LinearBwdCall& c, hipStream_t stream);

@@ -73,6 +73,10 @@ struct Part {
 };
 constexpr unsigned kNowhere = 0x7fffffffu;   // an offset past every part's end
 constexpr int kNonTemporal = 2;
+// What the backward pass reads (z, codes) is written past the caches, and so is a y that would not be there any more when the next product
+// comes to it.  us, y of every size in the caches and past them, 1024 -> 4096 alone and with the product that reads it: 134 MB 153 and
+// 136, 270 and 248; 67 MB 70 and 65, 137 and 140; 34 MB 36 and 34, 70 and 73.
+constexpr size_t kFarBytes = 96u << 20;
 
 // A wavefront's kFA x kNB blocks of 16 features x 16 tokens, in fp32 until a result is rounded.  They go through LDS, 16 tokens at a time
 // (kArea such chunks where there is room), so that a lane holds eight consecutive features of a token: memory is read and written 16 bytes a
@@ -401,7 +405,8 @@ __device__ __forceinline__ void linear_tile(const LinearStart& p, const LinearAr
   f32x4 sum[S::kFA][S::kOutB];
   add_groups<S>(acc, sum, lds, group, wave, lane);
 
-  constexpr int kWaveArea = S::kLds / S::kAllWaves, kArea = std::min(S::kOutB, kWaveArea / (S::kFA * 1024));
+  constexpr int kWaveArea = S::kLds / S::kAllWaves / 1024 * 1024, kFit = std::min(S::kOutB, kWaveArea / (S::kFA * 1024));
+  constexpr int kArea = S::kOutB % kFit == 0 ? kFit : kFit - 1;
   __syncthreads();   // (everyone is done with the stages)
   finish<S::kFA, S::kOutB, kArea, kGrad>(p, a, sum, lds + wave_id * kWaveArea, t0 + (wb * S::kFB + group * S::kOutB) * 16, f0 + wa * S::kFA * 16);
 }
@@ -422,24 +427,24 @@ __global__ __launch_bounds__(S::kThreads, S::kAllWaves / 4 * S::kPerCU) void lin
 }
 
 template <class S>
-long tiles_of(const LinearArgs& a) {
-  return (a.T + (long)S::kRowsB - 1) / S::kRowsB * ((a.O + S::kRowsA - 1) / S::kRowsA);
-}
-
-template <class S, bool kGrad>
-hipError_t launch_product(LinearArgs a, hipStream_t stream) {
+void deal_tiles(LinearArgs& a) {
   TileDeal& d = a.deal;
   d.tokens = (int)((a.T + (long)S::kRowsB - 1) / S::kRowsB);
   d.features = (a.O + S::kRowsA - 1) / S::kRowsA;
   d.by_feature = a.O > a.T && d.features >= 8;   // (every XCD reads all of the other operand: the smaller one)
   d.rows = (d.by_feature ? d.features : d.tokens) / 8;
+  a.far = (size_t)a.T * a.O * 2 > kFarBytes;
+}
+template <class S, bool kGrad>
+hipError_t launch_product(LinearArgs a, hipStream_t stream) {
+  deal_tiles<S>(a);
+  const TileDeal& d = a.deal;
   const int x = d.grid_x();
   int range_rows = 0;
   if (a.ranges.splits) {
     range_rows = (int)(std::max<size_t>(1, std::min<size_t>(1024 * 256 / S::kThreads, a.ranges.n / 4 / S::kThreads)) + x - 1) / x;
     a.ranges.blocks = range_rows * x;
   }
-  a.far = (size_t)a.T * a.O * 2 > (96u << 20);
   const int y = d.grid_y() + range_rows;
   const dim3 grid(x, std::min(y, kMostGridY), (y + kMostGridY - 1) / kMostGridY);
   const hipError_t e = allow_lds<&linear_kernel<S, kGrad>>(S::kLds);
@@ -449,32 +454,32 @@ hipError_t launch_product(LinearArgs a, hipStream_t stream) {
   return hipGetLastError();
 }
 
+// Which shape: a compute unit that gets n tiles of one needs about (k / 64) (c2 for every two tiles, c1 for an odd last one) + e n us.
 //                        features x tokens, wavefronts, stages, workgroups per CU, groups
 using Tile256 = Shape<4, 4, 2, 4, 2, 1>;
 using Tile128 = Shape<2, 2, 2, 2, 2, 2>;
 using Tile128x2 = Shape<2, 2, 2, 2, 2, 1, 2>;
 using Tile64 = Shape<2, 1, 2, 2, 3, 2>;
 using Tile64x2 = Shape<2, 1, 2, 2, 3, 1, 2>;
+struct ProductChoice {
+  double cost, tile_cost;   // us, and of a tile alone on its unit
+  long tiles;
+  int rows, groups;         // tokens of a tile; shapes with as many groups add up a product's stages in the same order
+  hipError_t (*launch)(LinearArgs, hipStream_t);
+};
+template <class S, bool kGrad>
+ProductChoice product_as(int T, int O, int K, double c1, double c2, double e) {
+  const long tiles = (T + (long)S::kRowsB - 1) / S::kRowsB * ((O + S::kRowsA - 1) / S::kRowsA), n = (tiles + 255) / 256;
+  const int stages = (K + 63) / 64;
+  return {stages * ((n / 2) * c2 + (n % 2) * c1) + e * n, stages * c1 + e, tiles, S::kRowsB, S::kGroups, launch_product<S, kGrad>};
+}
 template <bool kGrad>
-hipError_t run_product(const LinearArgs& a, hipStream_t stream) {
-  typedef hipError_t (*Launch)(LinearArgs, hipStream_t);
-  double best = 1e30;
-  Launch launch = nullptr;
-  auto offer = [&](auto shape, double c1, double c2, double e) {
-    typedef decltype(shape) S;
-    const long n = (tiles_of<S>(a) + 255) / 256;
-    const double cost = (a.K + 63) / 64 * ((n / 2) * c2 + (n % 2) * c1) + e * n;
-    if (cost < best) {
-      best = cost;
-      launch = launch_product<S, kGrad>;
-    }
-  };
-  offer(Tile256(), 1.37, 3.14, 5.33);
-  offer(Tile128(), 0.62, 1.09, 1.1);
-  offer(Tile128x2(), 0.47, 1.2, 1.86);
-  offer(Tile64(), 0.46, 0.74, 0.53);
-  offer(Tile64x2(), 0.39, 0.8, 0.71);
-  return launch(a, stream);
+ProductChoice choose_product(int T, int O, int K) {
+  ProductChoice best = product_as<Tile256, kGrad>(T, O, K, 1.37, 3.14, 5.33);
+  for (const ProductChoice& c : {product_as<Tile128, kGrad>(T, O, K, 0.62, 1.09, 1.1), product_as<Tile128x2, kGrad>(T, O, K, 0.47, 1.2, 1.86),
+                                 product_as<Tile64, kGrad>(T, O, K, 0.46, 0.74, 0.53), product_as<Tile64x2, kGrad>(T, O, K, 0.39, 0.8, 0.71)})
+    if (c.cost < best.cost) best = c;
+  return best;
 }
 
 // ---- few tokens ------------------------------------------------------------------------------------
@@ -596,41 +601,49 @@ hipError_t run_few(const LinearArgs& a, hipStream_t stream) {
 // Gradient with respect to the weights
 // ======================================================================================
 // Both operands are token-major, so their 64-token x 64-column tiles go into LDS as they are and both are read transposed.  A
-// workgroup owns a tile of dw and a range of the token blocks; partial sums of the ranges are added in a fixed order
-// afterwards (no atomics: the result is bit-reproducible).  The bias gradient rides along in the workgroups of the first
+// workgroup owns a tile of dw and a range of the token blocks; the ranges' sums are added in a fixed order (no atomic
+// additions: the result is bit-reproducible), in the launch (kMerge) or after it.  The bias gradient rides along in the workgroups of the first
 // column tile.  Rows of pad tokens are cleared in LDS after a block has landed, and blocks of padding only are skipped.
+// x in 8 bits (kCodes) passes through registers: 16 codes of a token and their scale become bf16, exactly, on the way to LDS.  That takes
+// a stage a third of a microsecond longer, in every tile that reads them; where a copy in bf16, written and read again, takes
+// less, the values are copied into the workspace first.  (us, dw with a copy and so: 16384 tokens, 4096 x 1024 178 and 151, 1024 x 4096 139 and 152,
+// 4072 tokens, 2048 x 768 36 and 59.)
 struct WeightGradArgs {
-  const unsigned short *g, *x;   // [T][F], [T][E]
+  const unsigned short* g;       // [T][F]
+  const void* x;                 // [T][E], bf16, or codes if x_scales is not null
+  const unsigned char* x_scales;
   const unsigned char* flags;    // [T] or null
-  float *out, *out_bias;         // [F][E], [F] or null (final when splits == 1)
-  float *part, *part_bias;       // [splits][F][E], [splits][F]
+  float *out, *out_bias;         // [F][E], [F] or null
+  float *part, *part_bias;       // the ranges' sums (splits > 1)
+  unsigned long long *arrived, ticket;
   int T, F, E;
   int splits, per_split;         // ranges of 64-token blocks
 };
-constexpr int kMostBlocks = 1024;   // of a range
+constexpr int kMostBlocks = 1024;      // of a range
+constexpr int kMergeBlocks = 160;      // of all ranges, where the launch adds them
 
-template <class S>
-__global__ __launch_bounds__(S::kThreads, S::kAllWaves / 4 * S::kPerCU) void linear_wgrad_kernel(WeightGradArgs a) {
-  extern __shared__ __attribute__((aligned(1024))) char lds[];
+template <class S, bool kMerge, bool kCodes>
+__device__ __forceinline__ void weight_grad_tile(const WeightGradArgs& a, char* lds, int workgroup) {
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave_id = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int group = wave_id / S::kWaves, wave = wave_id - group * S::kWaves;
   char* const ring = lds + group * S::kRingBytes;
-  const int e_tiles = (a.E + S::kRowsA - 1) / S::kRowsA, tiles = ((a.F + S::kRowsB - 1) / S::kRowsB) * e_tiles;
-  // XCD q = block % 8 takes a contiguous piece of the list ordered by token range first: workgroups that stream the same tokens share an L2
+  const int e_tiles = (a.E + S::kRowsA - 1) / S::kRowsA, f_tiles = (a.F + S::kRowsB - 1) / S::kRowsB, tiles = f_tiles * e_tiles;
+  // XCD q = workgroup % 8 takes a contiguous piece of the list ordered by token range first: workgroups that stream the same tokens share an L2
   const int total = tiles * a.splits, per_xcd = (total + 7) >> 3;
-  const int q = blockIdx.x & 7, jx = blockIdx.x >> 3, idx = q * per_xcd + jx;
+  const int q = workgroup & 7, jx = workgroup >> 3, idx = q * per_xcd + jx;
   if (jx >= per_xcd || idx >= total) return;
   const int split = idx / tiles, tile = idx - split * tiles;
   const int ft = tile / e_tiles, et = tile - ft * e_tiles;
   const int f0 = ft * S::kRowsB, e0 = et * S::kRowsA;
   const int wa = wave / S::kWB, wb = wave - wa * S::kWB;
   const int total_blocks = (int)((a.T + 63L) / 64);
-  const bool share = total_blocks <= kMostBlocks;   // every workgroup lists all blocks and takes its share of the live ones
+  constexpr int kList = kMerge ? kMergeBlocks : kMostBlocks;
+  const bool share = kMerge || total_blocks <= kList;   // every workgroup lists all blocks and takes its share of the live ones
   const int s_begin = share ? 0 : split * a.per_split, s_end = share ? total_blocks : min(total_blocks, s_begin + a.per_split);
 
-  __shared__ unsigned long long live_mask[kMostBlocks];   // pad tokens of the blocks with any other token, in order
-  __shared__ int live_block[kMostBlocks];
+  __shared__ unsigned long long live_mask[kList];   // pad tokens of the blocks with any other token, in order
+  __shared__ int live_block[kList];
   __shared__ int wave_live[S::kAllWaves];
   int n_live = 0;
   for (int s0 = s_begin; s0 < s_end; s0 += S::kThreads) {
@@ -657,37 +670,70 @@ __global__ __launch_bounds__(S::kThreads, S::kAllWaves / 4 * S::kPerCU) void lin
   }
   n_live = __builtin_amdgcn_readfirstlane(n_live);
   const int i_begin = share ? n_live * split / a.splits : 0, i_end = share ? n_live * (split + 1) / a.splits : n_live;
+  const int last_block = total_blocks - 1, last_rows = a.T - 64 * last_block;
 
-  // ---- operand streams: X tiles (columns e0 ..) then G tiles (columns f0 ..); columns past the last eight repeat those and are not stored
+  // ---- operand streams: X tiles (columns e0 ..) then G tiles (columns f0 ..); columns past the last eight repeat those and are not
+  // stored, rows past the end repeat the last one and are cleared like pad rows
   const unsigned x_stride = (unsigned)a.E * 2, g_stride = (unsigned)a.F * 2;
+  constexpr int kFirst = kCodes ? S::kLoadsA : 0;   // loads that go straight to LDS
   unsigned off[S::kLoads];
 #pragma unroll
-  for (int i = 0; i < S::kLoads; ++i) {
+  for (int i = kFirst; i < S::kLoads; ++i) {
     const bool is_x = i < S::kLoadsA;
     const LoadUnit l = load_unit<S::kWaves>(wave, lane, is_x ? i : i - S::kLoadsA);
     off[i] = (unsigned)l.row * (is_x ? x_stride : g_stride) + (unsigned)min((is_x ? e0 : f0) + 64 * l.tile + 8 * l.chunk, (is_x ? a.E : a.F) - 8) * 2;
   }
-  const int last_block = total_blocks - 1, last_rows = a.T - 64 * last_block;
-  const char *x_base = nullptr, *g_base = nullptr;   // of the stage being loaded
-  bool at_end = false;
-  auto prepare_block = [&](int block) {
-    block = __builtin_amdgcn_readfirstlane(block);
-    x_base = uniform_ptr(reinterpret_cast<const char*>(a.x) + (size_t)block * 64 * x_stride);
-    g_base = uniform_ptr(reinterpret_cast<const char*>(a.g) + (size_t)block * 64 * g_stride);
-    at_end = block == last_block;
-  };
-  auto load_one = [&](int slot, int i) {
-    const bool is_x = i < S::kLoadsA;
-    const int y = is_x ? i : i - S::kLoadsA;
-    unsigned o = off[i];
-    if (__builtin_expect(at_end, 0))   // rows past the end repeat the last one, and are cleared like pad rows
-      o -= (unsigned)max(0, load_unit<S::kWaves>(wave, lane, y).row - (last_rows - 1)) * (is_x ? x_stride : g_stride);
-    load_to_lds_16(is_x ? x_base : g_base, o, ring + slot * S::kStageBytes + (is_x ? 0 : S::kA * kTileBytes) + load_dst<S::kWaves>(wave, y));
-  };
   auto issue_stage = [&](int block, int slot) {
-    prepare_block(block);
+    char* st = ring + slot * S::kStageBytes;
+    block = __builtin_amdgcn_readfirstlane(block);
+    const char* const x_base = uniform_ptr(static_cast<const char*>(a.x) + (size_t)block * 64 * x_stride);
+    const char* const g_base = uniform_ptr(reinterpret_cast<const char*>(a.g) + (size_t)block * 64 * g_stride);
 #pragma unroll
-    for (int i = 0; i < S::kLoads; ++i) load_one(slot, i);
+    for (int i = kFirst; i < S::kLoads; ++i) {
+      const bool is_x = i < S::kLoadsA;
+      const int y = is_x ? i : i - S::kLoadsA;
+      unsigned o = off[i];
+      if (block == last_block) o -= (unsigned)max(0, load_unit<S::kWaves>(wave, lane, y).row - (last_rows - 1)) * (is_x ? x_stride : g_stride);
+      load_to_lds_16(is_x ? x_base : g_base, o, st + (is_x ? 0 : S::kA * kTileBytes) + load_dst<S::kWaves>(wave, y));
+    }
+  };
+  // Codes: a lane has 16 columns of a row, kUnits times; four lanes a row, sixteen rows and one tile of 64 columns a wavefront.
+  constexpr int kUnits = kCodes ? S::kA * 4 / S::kWaves : 0, kUnitsHere = kCodes ? kUnits : 1;
+  static_assert(!kCodes || (S::kA * 4 % S::kWaves == 0 && S::kStages == 2), "codes divide evenly, and are one stage ahead of their values");
+  struct Raw { unsigned w[4], scale; } raw[kUnitsHere];
+  const int scales = scale_blocks(a.E);
+  auto unit_tile = [&](int u) { return (wave + S::kWaves * u) >> 2; };
+  auto unit_row = [&](int u) { return ((wave + S::kWaves * u) & 3) * 16 + (lane >> 2); };
+  auto unit_column = [&](int u) { return e0 + 64 * unit_tile(u) + 16 * (lane & 3); };
+  auto read_codes = [&](int block) {
+    block = __builtin_amdgcn_readfirstlane(block);
+    const unsigned char* const base = static_cast<const unsigned char*>(a.x) + (size_t)block * 64 * a.E;
+    const unsigned char* const scale_base = a.x_scales + (size_t)block * 64 * scales;
+    const int most = block == last_block ? last_rows - 1 : 63;
+#pragma unroll
+    for (int u = 0; u < kUnits; ++u) {
+      const int row = min(unit_row(u), most), column = unit_column(u);
+      // (rows begin at multiples of 8: two halves, the second one past the row's end repeats the last eight)
+      const uint2 lo = *reinterpret_cast<const uint2*>(base + (unsigned)row * (unsigned)a.E + min(column, a.E - 8));
+      const uint2 hi = *reinterpret_cast<const uint2*>(base + (unsigned)row * (unsigned)a.E + min(column + 8, a.E - 8));
+      raw[u].w[0] = lo.x; raw[u].w[1] = lo.y; raw[u].w[2] = hi.x; raw[u].w[3] = hi.y;
+      raw[u].scale = scale_base[(unsigned)row * (unsigned)scales + min(column, a.E - 8) / kScaleBlock];
+    }
+  };
+  auto write_values = [&](unsigned long long padmask, int slot) {
+    char* const st = ring + slot * S::kStageBytes;
+#pragma unroll
+    for (int u = 0; u < kUnits; ++u) {
+      const int row = unit_row(u), chunk = 2 * (lane & 3);
+      const bool pad = (padmask >> row) & 1ull;
+      const float scale = scale_value(raw[u].scale);
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const uint2 lo = bf16_from_codes(raw[u].w[2 * h], scale), hi = bf16_from_codes(raw[u].w[2 * h + 1], scale);
+        const uint4 v = pad ? make_uint4(0, 0, 0, 0) : make_uint4(lo.x, lo.y, hi.x, hi.y);
+        *reinterpret_cast<uint4*>(st + unit_tile(u) * kTileBytes + row * 128 + (((chunk + h) ^ swz(row & 15)) << 4)) = v;
+      }
+    }
   };
 
   f32x4 acc[S::kFA][S::kFB];
@@ -702,52 +748,61 @@ __global__ __launch_bounds__(S::kThreads, S::kAllWaves / 4 * S::kPerCU) void lin
   FragOffsets fo;
   frag_offsets<true>(fo, lane);
 
-  constexpr bool kPipelined = S::kGroups == 1 && S::kStages == 2;
+  // this group's blocks: i_begin + group, + kGroups, ...  (An odd last block leaves group 1 a block of padding only.)
+  auto pads_of = [&](int i) { return i < i_end ? live_mask[min(i, i_end - 1)] : ~0ull; };
 #pragma unroll
-  for (int k = 0; k + (kPipelined ? 0 : 1) < S::kStages; ++k)
+  for (int k = 0; k + 1 < S::kStages; ++k)
     if (i_begin + group + k * S::kGroups < i_end) issue_stage(live_block[i_begin + group + k * S::kGroups], k);
+  auto block_at = [&](int i) { return live_block[min(i, i_end - 1)]; };
+  if (kCodes && i_begin < i_end) {
+    read_codes(block_at(i_begin + group));
+    write_values(pads_of(i_begin + group), 0);
+    read_codes(block_at(i_begin + group + S::kGroups));
+  }
   auto land = [&](int i, int it) {
-    if (!kPipelined) wait_vmcnt_le<S::kLoads * (S::kStages - 2)>(max(0, min(S::kStages - 2, (i_end - 1 - i) / S::kGroups)) * S::kLoads);
-    const unsigned long long padmask = S::kGroups == 1 || i < i_end ? live_mask[i] : ~0ull;   // (an odd last block leaves group 1 padding only)
+    wait_vmcnt_le<S::kLoads * (S::kStages - 2)>(max(0, min(S::kStages - 2, (i_end - 1 - i) / S::kGroups)) * S::kLoads);
+    const unsigned long long padmask = pads_of(i);
     if (padmask) {
       char* st = ring + (it % S::kStages) * S::kStageBytes;
 #pragma unroll
-      for (int l = 0; l < S::kLoads; ++l) {
+      for (int l = kFirst; l < S::kLoads; ++l) {
         const int y = l < S::kLoadsA ? l : l - S::kLoadsA;
         if ((padmask >> load_unit<S::kWaves>(wave, lane, y).row) & 1ull)
           *reinterpret_cast<uint4*>(st + (l < S::kLoadsA ? 0 : S::kA * kTileBytes) + load_dst<S::kWaves>(wave, y) + lane * 16) =
               make_uint4(0, 0, 0, 0);
       }
-      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     }
+    if (padmask || kCodes) asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
   };
-  auto add_bias = [&](const bf16x8 (&g)[S::kFB]) {
-    if (do_bias) {
+  if (S::kAlternate && group == 1) barrier_no_fence();  // group 1 follows one barrier behind
+  for (int i0 = i_begin, it = 0; i0 < i_end; i0 += S::kGroups, ++it) {
+    const int i = i0 + group, ahead = i + (S::kStages - 1) * S::kGroups;
+    const int next = block_at(ahead), later = kCodes ? block_at(ahead + S::kGroups) : 0;
+    const unsigned long long next_pads = kCodes ? pads_of(ahead) : 0;
+    land(i, it);
+    barrier_no_fence();          // landed for everyone; and everyone is done with the block before it
+    contract_stage<S, true, true, false>(ring + (it % S::kStages) * S::kStageBytes, fo, fo, wa, wb, acc,
+                                         [&]() {
+                                           // (the codes have landed with this stage; behind loads to LDS, which the compiler does not
+                                           // see, it would wait for those as well)
+                                           if (kCodes && i0 + S::kGroups < i_end) write_values(next_pads, (it + 1) % S::kStages);
+                                           if (ahead < i_end) issue_stage(next, (it + S::kStages - 1) % S::kStages);
+                                           if (kCodes && i0 + S::kGroups < i_end) read_codes(later);
+                                         },
+                                         [&](const bf16x8 (&g)[S::kFB]) {
+                                           if (do_bias) {
 #pragma unroll
-      for (int j = 0; j < S::kFB; ++j) bias_acc[j] = sum8(g[j], bias_acc[j]);
-    }
-  };
-  if constexpr (kPipelined) {
-    if (i_begin < i_end)
-      contract_pipelined<S, true, true>(ring, i_end - i_begin, fo, fo, wa, wb, acc, [&](int s) { prepare_block(live_block[i_begin + s]); },
-                                        [&](int s, int i) { load_one(s & 1, i); }, [&](int s) { land(i_begin + s, s); }, add_bias);
-  } else {
-    if (S::kAlternate && group == 1) barrier_no_fence();  // group 1 follows one barrier behind
-    for (int i0 = i_begin, it = 0; i0 < i_end; i0 += S::kGroups, ++it) {
-      const int i = i0 + group, ahead = i + (S::kStages - 1) * S::kGroups;
-      const int next = live_block[min(ahead, i_end - 1)];
-      land(i, it);
-      barrier_no_fence();          // landed for everyone; and everyone is done with the block before it
-      contract_stage<S, true, true, false>(ring + (it % S::kStages) * S::kStageBytes, fo, fo, wa, wb, acc,
-                                           [&]() { if (ahead < i_end) issue_stage(next, (it + S::kStages - 1) % S::kStages); }, add_bias,
-                                           []() {}, []() {});
-    }
-    if (S::kAlternate && group == 0) barrier_no_fence();
+                                             for (int j = 0; j < S::kFB; ++j) bias_acc[j] = sum8(g[j], bias_acc[j]);
+                                           }
+                                         },
+                                         []() {}, []() {});
   }
+  if (S::kAlternate && group == 0) barrier_no_fence();
   f32x4 sum[S::kFA][S::kOutB];
   add_groups<S>(acc, sum, lds, group, wave, lane);
 
   const int r = lane & 15, quarter = lane >> 4;
+  float bias_sum[S::kFB];   // of row 16 j + r, in group 0's wavefronts of the first columns
   if (a.out_bias && et == 0) {
     if (S::kGroups > 1) {  // the other group's column sums
       float* x = reinterpret_cast<float*>(lds);
@@ -760,18 +815,25 @@ __global__ __launch_bounds__(S::kThreads, S::kAllWaves / 4 * S::kPerCU) void lin
 #pragma unroll
         for (int j = 0; j < S::kFB; ++j) bias_acc[j] += x[(wb * S::kFB + j) * 64 + lane];
     }
-    if (do_bias && !group) {
-      float* bd = a.splits > 1 ? a.part_bias + (size_t)split * a.F : a.out_bias;
 #pragma unroll
-      for (int j = 0; j < S::kFB; ++j) {
-        const float b = quad_sum(bias_acc[j]);
-        const int f = f0 + (wb * S::kFB + j) * 16 + r;
-        if (quarter == 0 && f < a.F) bd[f] = b;
-      }
+    for (int j = 0; j < S::kFB; ++j) bias_sum[j] = quad_sum(bias_acc[j]);
+  }
+  const bool has_bias = do_bias && !group;
+  if constexpr (kMerge) {
+    const RangeMerge m = {a.part, a.part_bias, a.arrived, a.ticket, a.splits, tiles, f_tiles * S::kRowsB};
+    if (a.splits > 1 && !merge_ranges<S>(m, split, tile, f0 + wb * S::kFB * 16, has_bias, sum, bias_sum, wave_id)) return;
+  }
+  const bool partial = !kMerge && a.splits > 1;
+  if (has_bias) {
+    float* bd = partial ? a.part_bias + (size_t)split * a.F : a.out_bias;
+#pragma unroll
+    for (int j = 0; j < S::kFB; ++j) {
+      const int f = f0 + (wb * S::kFB + j) * 16 + r;
+      if (quarter == 0 && f < a.F) bd[f] = bias_sum[j];
     }
   }
   // a lane holds columns 16 i + 4 quarter .. + 3 of row 16 j + r
-  float* const to = (a.splits > 1 ? a.part + (size_t)split * a.F * a.E : a.out) + (size_t)f0 * a.E;
+  float* const to = (partial ? a.part + (size_t)split * a.F * a.E : a.out) + (size_t)f0 * a.E;
 #pragma unroll
   for (int j = 0; j < S::kOutB; ++j) {
     const int f = (wb * S::kFB + group * S::kOutB + j) * 16 + r;
@@ -782,47 +844,150 @@ __global__ __launch_bounds__(S::kThreads, S::kAllWaves / 4 * S::kPerCU) void lin
     }
   }
 }
+template <class S, bool kMerge, bool kCodes>
+__global__ __launch_bounds__(S::kThreads, S::kAllWaves / 4 * S::kPerCU) void weight_grad_kernel(WeightGradArgs a) {
+  extern __shared__ __attribute__((aligned(1024))) char lds[];
+  weight_grad_tile<S, kMerge, kCodes>(a, lds, blockIdx.x);
+}
 
 // For a weight gradient that no product follows.
 __global__ __launch_bounds__(256) void add_weight_ranges_kernel(RangeSums s) { add_ranges(s, blockIdx.x, 256); }
 
-using Wgrad256 = Shape<4, 4, 2, 4, 2, 1>;
-using Wgrad128 = Shape<2, 2, 2, 2, 2, 1, 2>;
+using Wgrad256 = Shape<4, 4, 2, 4, 2, 1>;      // 256 x 256
+using Wgrad128 = Shape<2, 2, 2, 2, 2, 1, 2>;   // 128 x 128, two groups
+
+template <class S, bool kCodes>
+__global__ __launch_bounds__(S::kThreads, S::kAllWaves / 4) void linear_bwd_kernel(WeightGradArgs w, LinearArgs a, int w_groups) {
+  extern __shared__ __attribute__((aligned(1024))) char lds[];
+  static_assert(S::kThreads == Wgrad128::kThreads, "one workgroup size for both");
+  if ((int)blockIdx.x < w_groups) {
+    weight_grad_tile<Wgrad128, true, kCodes>(w, lds, blockIdx.x);
+  } else {
+    int x, token_tile, feature_tile;
+    const int y = uniform_div(blockIdx.x - w_groups, a.deal.grid_x(), x);
+    if (dealt_tile(a.deal, x, y, token_tile, feature_tile)) linear_tile<S, true>(a, a, lds, token_tile * S::kRowsB, feature_tile * S::kRowsA);
+  }
+}
 
 size_t align256(size_t n) { return (n + 255) & ~size_t(255); }
-struct WeightGradPlan {
-  int splits, per_split, tile;
-  size_t bias_off, total;
+long tiles_of_size(int F, int E, int tile) { return (long)((F + tile - 1) / tile) * ((E + tile - 1) / tile); }
+
+// How both gradients are computed.  It goes by the sizes, so that neither depends on whether the other one is wanted (or how x was kept).
+struct BackwardPlan {
+  bool one_launch;
+  int splits, per_split, tile;   // of dw
+  ProductChoice product;         // of dx
+  bool copy;                     // x in 8 bits is brought back first
+  size_t bias_off, words_off, copy_off, total;
 };
-WeightGradPlan plan_weight_grad(int T, int F, int E) {
-  WeightGradPlan p = {};
-  const int blocks = (int)((T + 63L) / 64);
+// When the last of `first` workgroups of t1 us and then `second` ones of t2 us ends, one at a time on each unit.
+double end_of_both(int first, double t1, long second, double t2) {
+  constexpr int kUnits = 256;
+  const int late = first % kUnits, early = kUnits - late;   // units that end the first kind a round later, or not
+  double early_at = first / kUnits * t1, late_at = early_at + t1, end = late ? late_at : early_at;
+  while (second > 0) {
+    const bool use_early = !late || early_at <= late_at;
+    double& at = use_early ? early_at : late_at;
+    at += t2;
+    second -= use_early ? early : late;
+    end = std::max(end, at);
+  }
+  return end;
+}
+BackwardPlan plan_backward(int T, int E, int F, bool codes) {
+  BackwardPlan p = {};
+  const long blocks = (T + 63L) / 64;
   constexpr int kSlots = 256;
-  double best = 1e30;
+  p.product = choose_product<true>(T, E, F);
+  // Two launches: large tiles read half as much per contraction, small ones need fewer ranges, and every range leaves an fp32
+  // matrix that is written and read again.  In us, one workgroup a compute unit: 1.45 a token block for 256 x 256, 0.58 for
+  // 128 x 128 with two groups, 1 per 6.5 MB of partial sums.  (Measured and so, both gradients: 4072 tokens 2048 -> 768 43.6 and 45, 768 -> 2048 41
+  // and 47, 2048 tokens 768 -> 768 22.0 and 21.5, 512 17.1 and 17.5, 512 tokens 1024 -> 4096 37 and 38.)
+  double two = 1e30;
   for (int tile : {256, 128}) {
-    const long tiles = (long)((F + tile - 1) / tile) * ((E + tile - 1) / tile);
+    const long tiles = tiles_of_size(F, E, tile);
     // enough workgroups for the chip, but ranges of at least eight token blocks
-    const int want = (int)std::max<long>({1, std::min(std::max(1L, kSlots / tiles), blocks / 8L), (blocks + kMostBlocks - 1L) / kMostBlocks});
-    const int per = (blocks + want - 1) / want, splits = (blocks + per - 1) / per;
+    const long want = std::max({1L, std::min(std::max(1L, kSlots / tiles), blocks / 8), (blocks + kMostBlocks - 1) / kMostBlocks});
+    const long per = (blocks + want - 1) / want, splits = (blocks + per - 1) / per;
     const double rounds = (double)((tiles * splits + kSlots - 1) / kSlots);
-    const double cost = rounds * per * (tile == 256 ? 1.9 : 0.7) + (splits > 1 ? splits * 8.0 * F * E / 5.2e6 : 0.0);
-    if (cost < best) {
-      best = cost;
+    const double cost = rounds * per * (tile == 256 ? 1.45 : 0.58) + (tile == 256 ? 3.5 : 0.0) + (splits > 1 ? splits * 8.0 * F * E / 6.5e6 : 0.0);
+    if (cost < two) {
+      two = cost;
       p.tile = tile;
-      p.per_split = per;
-      p.splits = splits;
+      p.per_split = (int)per;
+      p.splits = (int)splits;
     }
   }
-  p.bias_off = p.splits > 1 ? align256((size_t)p.splits * F * E * 4) : 0;
-  p.total = p.bias_off + (p.splits > 1 ? align256((size_t)p.splits * F * 4) : 0) + 256;
+  two += 7.5 + p.product.cost;
+  // One: the tiles of dw first, 128 x 128, each over all blocks or a few ranges of them that the launch adds; those of dx take the units that
+  // are left.  Only for a dx whose tiles two groups of wavefronts share: beside tiles of 256 x 256 those of dw take half as long again.  (us, as two
+  // launches and as one: 512 tokens 768 -> 768 17.1 and 10.4, 1024 768 -> 2048 26.9 and 16.5, 2048 768 -> 768 22.0 and 18.3, 4096 1024 -> 1024 35 and 28.)
+  const long tiles = tiles_of_size(F, E, 128);
+  if (blocks <= kMergeBlocks && p.product.groups == 2)
+    for (int ranges = 1; ranges <= kMaxRanges && tiles * ranges <= kSlots && (ranges == 1 || blocks >= 8 * ranges); ++ranges) {
+      const int first = (int)((tiles * ranges + 7) / 8 * 8);
+      double t1 = (0.44 + 0.12 * std::min(1.0, first / 256.0)) * ((blocks + ranges - 1) / ranges) + 5.1;
+      for (int r = 1; r < ranges; r *= 2) t1 += 2.7;   // one addition of pairs
+      for (const ProductChoice& c : {product_as<Tile128x2, true>(T, E, F, 0.38, 0, 3.1), product_as<Tile64x2, true>(T, E, F, 0.35, 0, 1.8)}) {
+        // (padding, which this leaves out, shortens long ranges most: several must be worth 16 %)
+        const double cost = (ranges > 1 ? 1.16 : 1.0) * (0.5 + end_of_both(first, t1, c.tiles, c.tile_cost));
+        if (cost < two) {
+          two = cost;
+          p.one_launch = true;
+          p.splits = ranges;
+          p.tile = 128;
+          p.per_split = (int)blocks;
+          p.product = c;
+        }
+      }
+    }
+  const long rows = (F + p.tile - 1) / p.tile * p.tile, columns = (E + p.tile - 1) / p.tile * p.tile;   // whole tiles
+  if (p.splits > 1) {
+    p.bias_off = align256((size_t)p.splits * rows * columns * 4);
+    p.words_off = p.bias_off + align256((size_t)p.splits * rows * 4);
+    p.total = p.words_off + (p.one_launch ? (size_t)tiles * kMaxRanges * 8 : 0);
+  }
+  p.copy_off = align256(p.total);
+  const double rounds = (double)((tiles_of_size(F, E, p.tile) * p.splits + kSlots - 1) / kSlots), stages = (double)((blocks + p.splits - 1) / p.splits);
+  p.copy = 0.36 * rounds * stages > 2.5 + 3.0 * T * E / 4.6e6;
+  p.total = p.copy_off + (p.copy && codes ? (size_t)T * E * 2 : 0) + 256;
   return p;
 }
-template <class S>
+
+template <class S, bool kMerge, bool kCodes>
 hipError_t launch_weight_grad(const WeightGradArgs& a, hipStream_t stream) {
-  const long tiles = (long)((a.F + S::kRowsB - 1) / S::kRowsB) * ((a.E + S::kRowsA - 1) / S::kRowsA);
-  const hipError_t e = allow_lds<&linear_wgrad_kernel<S>>(S::kLds);
+  const long tiles = tiles_of_size(a.F, a.E, S::kRowsA);
+  static_assert(S::kRowsA == S::kRowsB, "square tiles");
+  const hipError_t e = allow_lds<&weight_grad_kernel<S, kMerge, kCodes>>(S::kLds);
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(linear_wgrad_kernel<S>, dim3((unsigned)(8 * ((tiles * a.splits + 7) / 8))), dim3(S::kThreads), S::kLds, stream, a);
+  hipLaunchKernelGGL((weight_grad_kernel<S, kMerge, kCodes>), dim3((unsigned)(8 * ((tiles * a.splits + 7) / 8))), dim3(S::kThreads), S::kLds, stream, a);
+  return hipGetLastError();
+}
+template <class S, bool kCodes>
+hipError_t launch_both(const WeightGradArgs& w, LinearArgs a, hipStream_t stream) {
+  deal_tiles<S>(a);
+  const int w_groups = (int)((tiles_of_size(w.F, w.E, 128) * w.splits + 7) / 8 * 8);   // (whole rounds of XCDs, so that the products' tiles are dealt as ever)
+  constexpr int kLds = std::max(S::kLds, Wgrad128::kLds);
+  const hipError_t e = allow_lds<&linear_bwd_kernel<S, kCodes>>(kLds);
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL((linear_bwd_kernel<S, kCodes>), dim3(w_groups + a.deal.grid_x() * a.deal.grid_y()), dim3(S::kThreads), kLds, stream, w, a, w_groups);
+  return hipGetLastError();
+}
+template <bool kCodes>
+hipError_t run_backward(const BackwardPlan& p, const WeightGradArgs& w, LinearArgs a, hipStream_t stream) {
+  if (p.one_launch && w.out) {
+    if (!a.y) return launch_weight_grad<Wgrad128, true, kCodes>(w, stream);
+    return p.product.rows == 128 ? launch_both<Tile128x2, kCodes>(w, a, stream) : launch_both<Tile64x2, kCodes>(w, a, stream);
+  }
+  if (w.out) {
+    const hipError_t e = p.tile == 256 ? launch_weight_grad<Wgrad256, false, kCodes>(w, stream) : launch_weight_grad<Wgrad128, false, kCodes>(w, stream);
+    if (e != hipSuccess) return e;
+    if (p.splits > 1) a.ranges = {w.part, w.part_bias, w.out, w.out_bias, (size_t)w.F * w.E, w.F, p.splits, 0};
+  }
+  if (a.y) return p.product.launch(a, stream);
+  if (!a.ranges.splits) return hipSuccess;
+  a.ranges.blocks = (int)std::max<size_t>(1, std::min<size_t>(1024, a.ranges.n / 4 / 256));
+  hipLaunchKernelGGL(add_weight_ranges_kernel, dim3(a.ranges.blocks), dim3(256), 0, stream, a.ranges);
   return hipGetLastError();
 }
 
@@ -843,56 +1008,46 @@ hipError_t launch_linear(const LinearCall& c, hipStream_t stream) {
   a.y_codes = c.y_codes;
   a.y_scales = c.y_scales;
   if (a.T <= kFewTokens && !a.z_scales && !a.y_codes) return run_few(a, stream);
-  return run_product<false>(a, stream);
+  return choose_product<false>(a.T, a.O, a.K).launch(a, stream);
 }
 
-size_t linear_bwd_workspace(int T, int E, int F, bool codes) {
-  return plan_weight_grad(T, F, E).total + (codes ? align256((size_t)T * E * 2) : 0) + 16;   // (the caller's address may be any)
-}
+size_t linear_bwd_workspace(int T, int E, int F, bool codes) { return plan_backward(T, E, F, codes).total; }   // (the caller's address may be any)
 
 hipError_t launch_linear_bwd(const LinearBwdCall& c, hipStream_t stream) {
+  const BackwardPlan p = plan_backward(c.T, c.E, c.F, c.x_scales != nullptr);
   LinearArgs a = {};
-  if (c.dw) {
-    const WeightGradPlan p = plan_weight_grad(c.T, c.F, c.E);
-    char* ws = static_cast<char*>(c.workspace);
-    ws += -reinterpret_cast<uintptr_t>(ws) & 15;
-    WeightGradArgs w = {};
-    w.g = static_cast<const unsigned short*>(c.dy);
-    w.x = static_cast<const unsigned short*>(c.x);
-    if (c.x_scales) {
-      void* values = ws + p.total;
-      const hipError_t e = launch_checkpoint_unpack(static_cast<const unsigned char*>(c.x), c.x_scales, c.T, c.E, false, values, stream);
-      if (e != hipSuccess) return e;
-      w.x = static_cast<const unsigned short*>(values);
-    }
-    w.flags = c.flags;
-    w.out = c.dw;
-    w.out_bias = c.dbias;
-    w.T = c.T; w.F = c.F; w.E = c.E;
-    w.splits = p.splits;
-    w.per_split = p.per_split;
-    w.part = reinterpret_cast<float*>(ws);
-    w.part_bias = reinterpret_cast<float*>(ws + p.bias_off);
-    const hipError_t e = p.tile == 256 ? launch_weight_grad<Wgrad256>(w, stream) : launch_weight_grad<Wgrad128>(w, stream);
-    if (e != hipSuccess) return e;
-    if (p.splits > 1) a.ranges = {w.part, w.part_bias, w.out, w.out_bias, (size_t)c.F * c.E, c.F, p.splits, 0};
-  }
-  if (!c.dx) {
-    if (!a.ranges.splits) return hipSuccess;
-    a.ranges.blocks = (int)std::max<size_t>(1, std::min<size_t>(1024, a.ranges.n / 4 / 256));
-    hipLaunchKernelGGL(add_weight_ranges_kernel, dim3(a.ranges.blocks), dim3(256), 0, stream, a.ranges);
-    return hipGetLastError();
-  }
   a.w = static_cast<const unsigned short*>(c.w);
   a.tok = static_cast<const unsigned short*>(c.dy);
   a.T = c.T; a.O = c.E; a.K = c.F;
   a.flags = c.flags;
   a.add = static_cast<const unsigned short*>(c.residual);
-  a.act = c.z ? c.act : kActNone;
+  a.act = c.act;
   a.z_in = c.z;
   a.z_in_scales = c.z_scales;
   a.y = static_cast<unsigned short*>(c.dx);
-  return run_product<true>(a, stream);
+  WeightGradArgs w = {};
+  w.g = static_cast<const unsigned short*>(c.dy);
+  w.x = c.x;
+  w.x_scales = c.x_scales;
+  w.flags = c.flags;
+  w.out = c.dw;
+  w.out_bias = c.dbias;
+  w.T = c.T; w.F = c.F; w.E = c.E;
+  w.splits = p.splits;
+  w.per_split = p.per_split;
+  w.ticket = c.ticket;
+  char* ws = static_cast<char*>(c.workspace);
+  ws += -reinterpret_cast<uintptr_t>(ws) & 15;
+  w.part = reinterpret_cast<float*>(ws);
+  w.part_bias = reinterpret_cast<float*>(ws + p.bias_off);
+  w.arrived = reinterpret_cast<unsigned long long*>(ws + p.words_off);
+  if (c.dw && c.x_scales && p.copy) {
+    const hipError_t e = launch_checkpoint_unpack(static_cast<const unsigned char*>(c.x), c.x_scales, c.T, c.E, false, ws + p.copy_off, stream);
+    if (e != hipSuccess) return e;
+    w.x = ws + p.copy_off;
+    w.x_scales = nullptr;
+  }
+  return w.x_scales ? run_backward<true>(p, w, a, stream) : run_backward<false>(p, w, a, stream);
 }
 
 }  // namespace mate

@@ -5,6 +5,7 @@
 
 #include <type_traits>
 
+#include "arrival.h"
 #include "d2l.h"
 #include "mfma_common.h"
 
@@ -237,6 +238,69 @@ __device__ __forceinline__ void add_ranges(const RangeSums& s, int block, int th
       for (int k = 1; k < s.splits; ++k) v += s.part_bias[(size_t)k * s.n_bias + i];
       s.out_bias[i] = v;
     }
+}
+
+// The same inside the launch: the range of a tile that is done last adds them all.
+constexpr int kMaxRanges = 8;
+struct RangeMerge {
+  float* part;                  // [splits][tiles][the tile's registers]
+  float* part_bias;             // [splits][bias_stride]
+  unsigned long long* arrived;  // [tiles][kMaxRanges]
+  unsigned long long ticket;    // see arrival.h
+  int splits, tiles, bias_stride;
+};
+// Ranges are added in pairs, pairs of pairs and so on: of two, the one that comes first leaves its registers
+// as they are ([wavefront][block][half][lane] pairs, in the place of its lowest range) and ends, the other adds
+// them to its own.  (One workgroup that adds all of them waits for 64 KB of far memory per range.)  False: this workgroup has left its own.
+// `row`: first row of the wavefront's blocks of B, whose sums `bias_sum` are if it has any.
+template <class S>
+__device__ __forceinline__ bool merge_ranges(const RangeMerge& m, int split, int tile, int row, bool has_bias, f32x4 (&sum)[S::kFA][S::kOutB],
+                                             float (&bias_sum)[S::kFB], int wave_id) {
+  constexpr int kTile = S::kRowsA * S::kRowsB, kBlocks = S::kFA * S::kOutB;
+  static_assert(kTile == S::kAllWaves * kBlocks * 256, "the registers are the tile");
+  const int tid = threadIdx.x, lane = tid & 63, r = lane & 15, quarter = lane >> 4;
+  __shared__ int second;
+  for (int level = 0; (1 << level) < m.splits; ++level) {
+    const int node = split >> level, other = (node ^ 1) << level;
+    if (other >= m.splits) continue;
+    unsigned long long* const word = m.arrived + (size_t)tile * kMaxRanges + (kMaxRanges - (kMaxRanges >> level)) + (node >> 1);
+    auto place = [&](int range) { return m.part + ((size_t)range * m.tiles + tile) * kTile + wave_id * kBlocks * 256 + lane * 2; };
+    auto bias_place = [&](int range) { return m.part_bias + (size_t)range * m.bias_stride + row + r; };
+    if (tid == 0) second = __hip_atomic_load(word, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == m.ticket;
+    __syncthreads();
+    if (!second) {
+      float* const mine = place(node << level);
+#pragma unroll
+      for (int y = 0; y < kBlocks; ++y)
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+          put_pair<true>(mine + y * 256 + h * 128, sum[y / S::kOutB][y % S::kOutB][2 * h], sum[y / S::kOutB][y % S::kOutB][2 * h + 1]);
+      if (has_bias && quarter == 0)
+#pragma unroll
+        for (int j = 0; j < S::kFB; ++j)
+          __hip_atomic_store(bias_place(node << level) + j * 16, bias_sum[j], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      publish_partials();
+      if (tid == 0) second = __hip_atomic_exchange(word, m.ticket, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == m.ticket;
+      __syncthreads();
+      if (!second) return false;
+    }
+    const float* const theirs = place(other);
+    float2 v[kBlocks][2];
+#pragma unroll
+    for (int y = 0; y < kBlocks; ++y)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) v[y][h] = get_pair<true>(theirs + y * 256 + h * 128);
+#pragma unroll
+    for (int y = 0; y < kBlocks; ++y) sum[y / S::kOutB][y % S::kOutB] += f32x4{v[y][0].x, v[y][0].y, v[y][1].x, v[y][1].y};
+    if (has_bias)
+#pragma unroll
+      for (int j = 0; j < S::kFB; ++j)
+        bias_sum[j] += __hip_atomic_load(bias_place(other) + j * 16, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    // (cleared again, so that a captured launch, which is replayed with its old ticket, finds none of its own)
+    if (tid == 0) __hip_atomic_store(word, 0ull, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    __syncthreads();  // (everyone has looked at `second`)
+  }
+  return true;
 }
 
 // Which of the 64 tokens from position n0 of the sequence at flags[seq] on are padding (or past its end):

@@ -394,7 +394,6 @@ struct WgradArgs {
   int want_bias;
 };
 constexpr int kMaxRange = 1024;   // token blocks of one range
-constexpr int kMaxRanges = 8;     // of a launch that adds them itself
 
 // kList: token blocks of one range at most.  kChain > 0: a group's accumulators go into a second set after every
 // kChain blocks, so that a long range is no less exact than the sum of short ones.
@@ -599,54 +598,8 @@ __device__ __forceinline__ void wgrad_tile(WgradArgs a, char* lds, int block) {
   }
   const bool has_bias = do_bias && !group;
   if constexpr (kMerge) {
-    if (a.splits > 1) {
-      // Ranges are added in pairs, pairs of pairs and so on: of two, the one that comes first leaves its registers
-      // as they are ([wavefront][block][half][lane] pairs, in the place of its lowest range) and ends, the other adds
-      // them to its own.  (One workgroup that adds all of them waits for 64 KB of far memory per range.)
-      constexpr int kTile = S::kRowsA * S::kRowsB, kBlocks = S::kFA * S::kOutB;
-      static_assert(kTile == S::kAllWaves * kBlocks * 256, "the registers are the tile");
-      __shared__ int second;
-      for (int level = 0; (1 << level) < a.splits; ++level) {
-        const int node = split >> level, other = (node ^ 1) << level;
-        if (other >= a.splits) continue;
-        unsigned long long* const word = a.arrived + (size_t)tile * kMaxRanges + (kMaxRanges - (kMaxRanges >> level)) + (node >> 1);
-        auto place = [&](int range) { return a.part + ((size_t)range * tiles + tile) * kTile + wave_id * kBlocks * 256 + lane * 2; };
-        auto bias_place = [&](int range) { return a.part_bias + (size_t)range * a.F + f0 + wb * S::kFB * 16 + r; };
-        if (tid == 0) second = __hip_atomic_load(word, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == a.ticket;
-        __syncthreads();
-        if (!second) {
-          float* const mine = place(node << level);
-#pragma unroll
-          for (int y = 0; y < kBlocks; ++y)
-#pragma unroll
-            for (int h = 0; h < 2; ++h)
-              put_pair<true>(mine + y * 256 + h * 128, sum[y / S::kOutB][y % S::kOutB][2 * h], sum[y / S::kOutB][y % S::kOutB][2 * h + 1]);
-          if (has_bias && quarter == 0)
-#pragma unroll
-            for (int j = 0; j < S::kFB; ++j)
-              __hip_atomic_store(bias_place(node << level) + j * 16, bias_sum[j], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-          publish_partials();
-          if (tid == 0) second = __hip_atomic_exchange(word, a.ticket, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == a.ticket;
-          __syncthreads();
-          if (!second) return;
-        }
-        const float* const theirs = place(other);
-        float2 v[kBlocks][2];
-#pragma unroll
-        for (int y = 0; y < kBlocks; ++y)
-#pragma unroll
-          for (int h = 0; h < 2; ++h) v[y][h] = get_pair<true>(theirs + y * 256 + h * 128);
-#pragma unroll
-        for (int y = 0; y < kBlocks; ++y) sum[y / S::kOutB][y % S::kOutB] += f32x4{v[y][0].x, v[y][0].y, v[y][1].x, v[y][1].y};
-        if (has_bias)
-#pragma unroll
-          for (int j = 0; j < S::kFB; ++j)
-            bias_sum[j] += __hip_atomic_load(bias_place(other) + j * 16, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        // (cleared again, so that a captured launch, which is replayed with its old ticket, finds none of its own)
-        if (tid == 0) __hip_atomic_store(word, 0ull, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        __syncthreads();  // (everyone has looked at `second`)
-      }
-    }
+    const RangeMerge m = {a.part, a.part_bias, a.arrived, a.ticket, a.splits, tiles, a.F};
+    if (a.splits > 1 && !merge_ranges<S>(m, split, tile, f0 + wb * S::kFB * 16, has_bias, sum, bias_sum, wave_id)) return;
   }
   const bool partial = !kMerge && a.splits > 1;
   // a lane holds columns 16 i + 4 quarter .. + 3 of row 16 j + r
