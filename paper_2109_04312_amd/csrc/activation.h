@@ -9,7 +9,7 @@
 // F(-|z|) = 0.5 erfc(|z| / sqrt(2)) by formula 7.1.26 of Abramowitz and Stegun, t (a1 + .. + a5 t^4) e^(-z^2 / 2) with
 // t = 1 / (1 + 0.3275911 |z| / sqrt(2)), off by 1.5e-7 at most: no branch, one exponential, which the derivative's
 // density is as well, and an error that shrinks with e^(-z^2 / 2) in the tail instead of staying at an ulp of 1.
-// (A product's epilogue evaluates it for 67 million values of a large layer, 18 instruction slots each.)
+// (A product's epilogue evaluates it for 67 million values of a large layer, 19 instruction slots each.)
 #pragma once
 #include <hip/hip_runtime.h>
 
@@ -23,17 +23,16 @@ enum Activation { kActNone = 0, kActRelu = 1, kActGelu = 2, kActGeluTanh = 3, kA
 
 __device__ __forceinline__ float logistic(float u) { return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-kLog2e * u)); }
 
-// F(z) and e^(-z^2 / 2)
-struct Normal { float below, bell; };
+// F(-|z|) and e^(-z^2 / 2)
+struct Normal { float tail, bell; };
 __device__ __forceinline__ Normal normal(float z) {
   const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(0.3275911f * 0.70710678f, __builtin_fabsf(z), 1.f));
-  float s = __builtin_fmaf(t, 1.061405429f, -1.453152027f);
-  s = __builtin_fmaf(t, s, 1.421413741f);
-  s = __builtin_fmaf(t, s, -0.284496736f);
-  s = __builtin_fmaf(t, s, 0.254829592f);
+  float s = __builtin_fmaf(t, 0.5f * 1.061405429f, 0.5f * -1.453152027f);
+  s = __builtin_fmaf(t, s, 0.5f * 1.421413741f);
+  s = __builtin_fmaf(t, s, 0.5f * -0.284496736f);
+  s = __builtin_fmaf(t, s, 0.5f * 0.254829592f);
   const float bell = __builtin_amdgcn_exp2f(z * z * (-0.5f * kLog2e));
-  const float tail = 0.5f * t * s * bell;
-  return {z < 0.f ? tail : 1.f - tail, bell};
+  return {t * s * bell, bell};
 }
 
 // Is z above 0, or not a number?  (A comparison alone would lose a NaN in relu.)
@@ -47,7 +46,8 @@ constexpr float kTanhSlope = 1.5957691216057308f, kTanhCubic = 0.044715f * kTanh
 template <int kAct>
 __device__ __forceinline__ float activate(float z) {
   if constexpr (kAct == kActRelu) return passes(z) ? z : 0.f;
-  if constexpr (kAct == kActGelu) return z * normal(z).below;
+  // z F(z) = max(z, 0) - |z| F(-|z|).  (A NaN comes through F; where |z| is cut, F is zero, and infinity times zero would not be.)
+  if constexpr (kAct == kActGelu) return __builtin_fmaf(-__builtin_fminf(__builtin_fabsf(z), 64.f), normal(z).tail, __builtin_fmaxf(z, 0.f));
   if constexpr (kAct == kActGeluTanh) return z * logistic(z * __builtin_fmaf(kTanhCubic, z * z, kTanhSlope));
   if constexpr (kAct == kActSilu) return z * logistic(z);
   if constexpr (kAct == kActTanh) {
@@ -64,7 +64,7 @@ __device__ __forceinline__ float slope(float z) {
   if constexpr (kAct == kActRelu) return passes(z) ? 1.f : 0.f;
   if constexpr (kAct == kActGelu) {
     const Normal n = normal(z);
-    return __builtin_fmaf(zc * 0.3989422804f, n.bell, n.below);
+    return __builtin_fmaf(zc * 0.3989422804f, n.bell, z < 0.f ? n.tail : 1.f - n.tail);
   }
   if constexpr (kAct == kActGeluTanh || kAct == kActSilu) {
     const float p = logistic(kAct == kActSilu ? z : z * __builtin_fmaf(kTanhCubic, z * z, kTanhSlope));
