@@ -483,42 +483,51 @@ ProductChoice choose_product(int T, int O, int K) {
 }
 
 // ---- few tokens ------------------------------------------------------------------------------------
-// Up to 64 tokens: what takes time is reading the weights, and latency.  A workgroup has kRows features and all tokens; its wavefronts
-// share the contraction and read operands straight from memory into registers (a lane holds 16 of 64 terms, so that a row's 128
-// bytes are read together; both operands hold the same ones).  Their sums are added through LDS, in the order of the wavefronts.
-// A compute unit has only so many reads under way, so that all of them should share the weights: where 16 features a workgroup
-// leave units without one, a workgroup has 8 or 4, and the 16 rows of an operand are those at 2 or 4 places of the contraction, each
-// multiplied with the tokens at all of these places, of which one product in 2 or 4 counts (there is time for that).
-template <int kRows, int kFB, int kWaves>
-__global__ __launch_bounds__(64 * kWaves) void few_kernel(const unsigned short* w, const unsigned short* tok, int T, int O, int K, LinearArgs a) {
-  constexpr int kParts = 16 / kRows, kDepth = std::max(1, 4 / kParts / (kFB > 2 ? 2 : 1));   // kDepth: steps whose loads travel together
-  __shared__ f32x4 part[kWaves][kFB][64];
+// Where tiles of 128 features leave most units idle, what takes time is latency, and how much a unit can read at a time (some 35 GB/s).
+// A workgroup has 4 to 32 features and 16 to 64 tokens; its wavefronts share the contraction, each a piece of it, and read operands straight from
+// memory into registers.  Their sums are added through LDS, in the order of the wavefronts.
+// kRows < 16: where 16 features a workgroup leave units without one, a workgroup has 8 or 4, and the 16 rows of an operand are those at 2
+// or 4 places of the contraction, each multiplied with the tokens at all of these places, of which one product in 2 or 4 counts (there
+// is time for that).
+template <int kRows, int kFA, int kFB>
+__global__ __launch_bounds__(512) void few_kernel(const unsigned short* w, const unsigned short* tok, int T, int O, int K, LinearArgs a) {
+  constexpr int kWaves = 8, kParts = 16 / kRows, kBlocks = kFA * kFB;
+  constexpr int kDepth = std::max(1, 4 / kParts / (kFB > 2 ? 2 : 1) / kFA);   // steps whose loads travel together
+  static_assert((kParts == 1 || kFA == 1) && kBlocks <= kWaves, "a wavefront for each block of results");
+  __shared__ f32x4 part[kWaves][kBlocks][64];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, q = lane >> 4;
-  const int f0 = blockIdx.x * kRows;
-  const unsigned short *row_w = w + (size_t)min(f0 + r % kRows, O - 1) * K + 64 * (r / kRows) + 8 * q, *rows_x[kFB];
+  const int f0 = blockIdx.x * (kRows * kFA), t0 = blockIdx.y * (16 * kFB);
   const int first = 64 * (r / kRows) + 8 * q;   // of this lane's terms of the weights in a step
+  const unsigned short *rows_w[kFA], *rows_x[kFB];
 #pragma unroll
-  for (int j = 0; j < kFB; ++j) rows_x[j] = tok + (size_t)min(16 * j + r, T - 1) * K + 8 * q;
-  f32x4 acc[kParts][kFB];
+  for (int i = 0; i < kFA; ++i) rows_w[i] = w + (size_t)min(f0 + 16 * i + r % kRows, O - 1) * K + first;
+#pragma unroll
+  for (int j = 0; j < kFB; ++j) rows_x[j] = tok + (size_t)min(t0 + 16 * j + r, T - 1) * K + 8 * q;
+  f32x4 acc[kParts][kFA][kFB];
 #pragma unroll
   for (int s = 0; s < kParts; ++s)
 #pragma unroll
-    for (int j = 0; j < kFB; ++j) acc[s][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-  bf16x8 fw[kDepth][2], fx[kDepth][kParts][kFB][2];
+    for (int i = 0; i < kFA; ++i)
+#pragma unroll
+      for (int j = 0; j < kFB; ++j) acc[s][i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  bf16x8 fw[kDepth][kFA][2], fx[kDepth][kParts][kFB][2];
   auto multiply = [&](int d) {
 #pragma unroll
     for (int s = 0; s < kParts; ++s)
 #pragma unroll
       for (int h = 0; h < 2; ++h)
 #pragma unroll
-        for (int j = 0; j < kFB; ++j) acc[s][j] = mfma16_apart(fw[d][h], fx[d][s][j][h], acc[s][j]);
+        for (int i = 0; i < kFA; ++i)
+#pragma unroll
+          for (int j = 0; j < kFB; ++j) acc[s][i][j] = mfma16_apart(fw[d][i][h], fx[d][s][j][h], acc[s][i][j]);
   };
   constexpr int kTerms = 64 * kParts;   // of a step
   auto load = [&](int d, int c, auto&& one) {   // one(address, first term)
     const int at = c * kTerms;
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      fw[d][h] = one(row_w + at + 32 * h, at + first + 32 * h);
+#pragma unroll
+      for (int i = 0; i < kFA; ++i) fw[d][i][h] = one(rows_w[i] + at + 32 * h, at + first + 32 * h);
 #pragma unroll
       for (int s = 0; s < kParts; ++s)
 #pragma unroll
@@ -543,23 +552,25 @@ __global__ __launch_bounds__(64 * kWaves) void few_kernel(const unsigned short* 
   }
   // Rows 4 q .. + 3 of a product: kRows = 4: features 0 .. 3 at place q; 8: features 4 (q % 2) .. + 3 at place q / 2.
 #pragma unroll
-  for (int j = 0; j < kFB; ++j) {
-    f32x4 x = acc[0][j];
+  for (int i = 0; i < kFA; ++i)
 #pragma unroll
-    for (int s = 1; s < kParts; ++s)
+    for (int j = 0; j < kFB; ++j) {
+      f32x4 x = acc[0][i][j];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) x[e] = q * kParts / 4 == s ? acc[s][j][e] : x[e];
-    part[wave][j][lane] = x;
-  }
+      for (int s = 1; s < kParts; ++s)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[e] = q * kParts / 4 == s ? acc[s][i][j][e] : x[e];
+      part[wave][i * kFB + j][lane] = x;
+    }
   __syncthreads();
-  if (wave >= kFB) return;
+  if (wave >= kBlocks) return;
   f32x4 z = part[0][wave][lane];
 #pragma unroll
   for (int v = 1; v < kWaves; ++v) z += part[v][wave][lane];
   if (kParts > 1)
 #pragma unroll
     for (int e = 0; e < 4; ++e) z[e] = kParts == 4 ? quad_sum(z[e]) : half_sum(z[e]);
-  const int t = 16 * wave + r, f = f0 + 4 * q;   // a lane's four features of a token
+  const int i = wave / kFB, t = t0 + 16 * (wave - i * kFB) + r, f = f0 + 16 * i + 4 * q;   // a lane's four features of a token
   if (t >= T || f >= O || 4 * q >= kRows) return;
   const size_t at = (size_t)t * O + f;
   uint2 add = make_uint2(0, 0);
@@ -576,25 +587,33 @@ __global__ __launch_bounds__(64 * kWaves) void few_kernel(const unsigned short* 
   if (a.z) *reinterpret_cast<uint2*>(static_cast<unsigned short*>(a.z) + at) = make_uint2(pack2(z[0], z[1]), pack2(z[2], z[3]));
   *reinterpret_cast<uint2*>(a.y + at) = make_uint2(pack2(y[0], y[1]), pack2(y[2], y[3]));
 }
-template <int kRows, int kFB>
-hipError_t launch_few(const LinearArgs& a, hipStream_t stream) {
-  constexpr int kWaves = 8;
-  hipLaunchKernelGGL((few_kernel<kRows, kFB, kWaves>), dim3((a.O + kRows - 1) / kRows), dim3(64 * kWaves), 0, stream, a.w, a.tok, a.T, a.O, a.K, a);
+template <int kRows, int kFA, int kFB>
+hipError_t launch_few(LinearArgs a, hipStream_t stream) {
+  const dim3 grid((a.O + kRows * kFA - 1) / (kRows * kFA), (a.T + 16 * kFB - 1) / (16 * kFB));
+  hipLaunchKernelGGL((few_kernel<kRows, kFA, kFB>), grid, dim3(512), 0, stream, a.w, a.tok, a.T, a.O, a.K, a);
   return hipGetLastError();
 }
-template <int kRows>
-hipError_t launch_few(const LinearArgs& a, hipStream_t stream) {
-  if constexpr (kRows > 4)
-    if (a.T > 32) return launch_few<kRows, 4>(a, stream);
-  return a.T <= 16 ? launch_few<kRows, 1>(a, stream) : launch_few<kRows, 2>(a, stream);
+// us of a launch, beside those of tiles (which need three that their costs leave out): a unit reads its workgroups' rows at 35 GB/s.  Over 96
+// products of 1 to 1024 tokens and eight pairs of widths (in a graph, weights not in the L2) what it takes is 2 % behind the best form in the
+// mean, 24 % at most (where all take 3 to 4 us).  us, tiles and so: 1 token 768 -> 768 7.1 and 3.1, 128 8.0 and 4.5, 512 8.4 and 7.0; 1024 -> 4096 at 16
+// 8.2 and 4.7, at 64 8.9 and 6.5; 4096 -> 1024 at 1 21 and 4.7, at 256 22 and 17.
+struct FewChoice {
+  double cost;
+  hipError_t (*launch)(LinearArgs, hipStream_t);
+};
+template <int kRows, int kFA, int kFB>
+FewChoice few_as(int T, int O, int K) {
+  const long groups = (long)((O + kRows * kFA - 1) / (kRows * kFA)) * ((T + 16 * kFB - 1) / (16 * kFB));
+  const double bytes = 2.0 * K * (kRows * kFA + std::min(T, 16 * kFB));
+  return {2.6 + (double)((groups + 255) / 256) * bytes / 35e3, launch_few<kRows, kFA, kFB>};
 }
-// us (in a graph, weights not in the L2), 16, 8 and 4 features a workgroup: 4096 -> 1024 at 1 token 6.6, 5.4, 4.5, at 16 9.2, 7.7, 7.3, at 32 12.6, 11.2, 11.0;
-// 2048 -> 768 at 1 4.4, 3.6, 3.4; 1024 -> 1024 at 16 3.9, 3.7, 3.8; 1024 -> 4096 at 1 3.9, 4.3, 4.7, at 24 5.2, 6.7, 10.7 (and 8.6 as a product of tiles),
-// at 64 7.0, 10.8, 23.5 (8.9).
-constexpr int kFewTokens = 64;
-hipError_t run_few(const LinearArgs& a, hipStream_t stream) {
-  if (a.O > 2048) return launch_few<16>(a, stream);
-  return a.O > 1024 || a.T > 32 ? launch_few<8>(a, stream) : launch_few<4>(a, stream);
+constexpr int kFewTokens = 1024;   // (a grid's second dimension; more are never faster so)
+FewChoice choose_few(int T, int O, int K) {
+  FewChoice best = {1e30, nullptr};
+  for (const FewChoice& c : {few_as<4, 1, 1>(T, O, K), few_as<8, 1, 1>(T, O, K), few_as<16, 1, 1>(T, O, K), few_as<16, 1, 2>(T, O, K),
+                             few_as<16, 1, 4>(T, O, K), few_as<16, 2, 2>(T, O, K), few_as<16, 2, 4>(T, O, K)})
+    if (c.cost < best.cost) best = c;
+  return best;
 }
 
 // ======================================================================================
@@ -1007,8 +1026,12 @@ hipError_t launch_linear(const LinearCall& c, hipStream_t stream) {
   a.z_scales = c.z_scales;
   a.y_codes = c.y_codes;
   a.y_scales = c.y_scales;
-  if (a.T <= kFewTokens && !a.z_scales && !a.y_codes) return run_few(a, stream);
-  return choose_product<false>(a.T, a.O, a.K).launch(a, stream);
+  const ProductChoice tiles = choose_product<false>(a.T, a.O, a.K);
+  if (a.T <= kFewTokens && !a.z_scales && !a.y_codes) {
+    const FewChoice few = choose_few(a.T, a.O, a.K);
+    if (few.cost < tiles.cost + 3.0) return few.launch(a, stream);
+  }
+  return tiles.launch(a, stream);
 }
 
 size_t linear_bwd_workspace(int T, int E, int F, bool codes) { return plan_backward(T, E, F, codes).total; }   // (the caller's address may be any)
