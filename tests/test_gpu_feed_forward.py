@@ -477,3 +477,138 @@ def test_offsets_past_32_bits():
     wx = ff.linear_backward(g, x[-1:, -300:], w, flags[-1:, -300:])[0]
     e = sum_error(F, ff.zero_pads(g.double().abs(), flags[-1:, -300:]) @ w.double().abs())
     within(dx[-1:, -300:], wx, e + BF16 * (wx.abs() + e) + 1e-300, "dx")
+
+
+# ---- each form that sizes choose -----------------------------------------------------------------------
+# few tokens without 8 bits: 4, 8, 16 and 32 features by 16, 32 and 64 tokens a workgroup; contractions of less than a step, of whole
+# steps, with a rest for one of the eight wavefronts, and as wide as there is; a last token tile and feature tile that are not full
+@pytest.mark.parametrize("keep_z", [0, 1])
+@pytest.mark.parametrize("B,N,E,F", [(1, 1, 8, 8), (1, 7, 72, 776), (1, 1, 8, 1032), (5, 103, 136, 40), (1, 17, 264, 2048), (5, 13, 264, 1288),
+                                     (2, 20, 264, 4096), (7, 100, 72, 1032), (1, 515, 200, 776), (2, 512, 520, 136), (3, 1, 4104, 72),
+                                     (1, 9, 65536, 8), (3, 1, 8, 65536), (3, 11, 4096, 1024), (8, 125, 8, 8)])
+def test_few_tokens(B, N, E, F, keep_z):
+    check_forward(E + N, B, N, E, F, "silu" if keep_z else "gelu_tanh", padding="scattered" if keep_z else "tail", bias=N != 7, residual=N != 13,
+                  keep_z=keep_z, keep_y=False)
+
+
+# tiles of each size, with 8 bits of both, odd widths; and results that are written past the caches
+@pytest.mark.parametrize("B,N,E,F", [(9, 1000, 72, 1288), (3, 1500, 768, 776), (9, 1000, 8, 136), (3, 100, 264, 136), (2, 7, 1032, 264), (4, 4096, 64, 4096)])
+def test_products(B, N, E, F):
+    check_forward(N, B, N, E, F, "silu", padding="scattered", keep_z=1 if N > 3000 else 2)
+
+
+# both gradients in one launch, dx by tiles of 64 and of 128 tokens, dw in one to eight ranges of token blocks; and in two launches, dw by
+# tiles of 128 and of 256, in one range and several; from 16 bits, from 8 bits as they are and copied, with rows that end in half of 16 codes
+BACKWARDS = [(5, 13, 72, 2048), (2, 65, 264, 136), (7, 100, 264, 520), (7, 100, 264, 1288), (4, 500, 520, 1032), (3, 1000, 520, 1032), (9, 500, 24, 4096),
+             (4, 500, 520, 520), (1, 2000, 136, 2048), (6, 1500, 24, 4096), (6, 1000, 264, 1032), (5, 1200, 200, 1288), (9, 500, 72, 2048),
+             (16, 1024, 136, 8), (4, 4096, 4096, 136), (9, 1000, 1032, 1288), (6, 1000, 264, 520), (3, 4000, 136, 776), (3, 1500, 4096, 520),
+             (1, 3, 65536, 8), (1, 3, 8, 65536), (1, 515, 4096, 4096), (2, 650, 2048, 264)]
+
+
+@pytest.mark.parametrize("x8", [False, True])
+@pytest.mark.parametrize("B,N,E,F", BACKWARDS)
+def test_gradients(B, N, E, F, x8):
+    check_backward(N, B, N, E, F, "silu", padding="scattered" if N % 2 else "tail", residual=N % 100 != 0, x8=x8, z8=not x8)
+
+
+@pytest.mark.parametrize("padding", [None, "all"])
+def test_gradients_without_and_of_nothing_but_padding(padding):
+    for B, N, E, F in ((2, 65, 264, 136), (4, 500, 520, 520), (9, 500, 72, 2048), (6, 1000, 264, 520)):
+        check_backward(N, B, N, E, F, "relu", padding=padding, x8=N == 500)
+
+
+def one_sequence_only(i, b):
+    """Every other sequence is padding: most ranges of token blocks have nothing."""
+    i.flags[:] = PAD
+    i.flags[b, 3:] = 0
+
+
+@pytest.mark.parametrize("B,N,E,F", [(9, 500, 72, 2048), (4, 500, 520, 520), (6, 1000, 264, 520)])
+def test_results_do_not_depend_on_what_else_is_wanted_or_running(B, N, E, F):
+    """Merged ranges and added ones, x in 8 bits and 16: either gradient alone has the same bits, from a workspace full of NaN at an odd address, and
+    while the same call runs on another stream with a workspace of its own."""
+    mate = mate_module()
+    i = Inputs(N, B, N, E, F, "scattered")
+    for x in (mate.checkpoint_pack(i.x), i.x):
+        kw = dict(z=i.z, act=mate.MATE_ACT_GELU, residual=i.res_x)
+        size = mate.mate_linear_bwd_workspace_bytes(B, N, E, F, int(x is not i.x))
+        want = mate.linear_bwd(i.dy, x, i.w, i.flags, **kw)
+        torch.cuda.synchronize()
+        streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+        spaces = [torch.full((size + 3,), 255, dtype=torch.uint8, device="cuda") for _ in streams]
+        torch.cuda.synchronize()
+        got = []
+        for _ in range(5):
+            for s, ws in zip(streams, spaces):
+                with torch.cuda.stream(s):
+                    got.append(mate.linear_bwd(i.dy, x, i.w, i.flags, ws=ws[3:], **kw))
+        torch.cuda.synchronize()
+        for g in got:
+            assert all(torch.equal(u, v) for u, v in zip(g, want))
+        only_x = mate.linear_bwd(i.dy, x, i.w, i.flags, want_dw=False, want_dbias=False, **kw)
+        only_w = mate.linear_bwd(i.dy, x, i.w, i.flags, want_dx=False, **kw)
+        assert torch.equal(only_x[0], want[0]) and torch.equal(only_w[1], want[1]) and torch.equal(only_w[2], want[2])
+        one_sequence_only(i, 1)
+        alone = mate.linear_bwd(i.dy[1:2].contiguous(), i.x[1:2].contiguous(), i.w, i.flags[1:2].contiguous(), z=i.z[1:2].contiguous(),
+                                act=mate.MATE_ACT_GELU, residual=i.res_x[1:2].contiguous())
+        among = mate.linear_bwd(i.dy, i.x, i.w, i.flags, **kw)
+        one = sum_error(N, i.dy[1].double().abs().T @ i.x[1].double().abs())
+        within(among[1], alone[1].double(), 2 * one + 1e-300, "dw of one sequence")
+
+
+@pytest.mark.parametrize("B,N,E,F", [(9, 500, 72, 2048), (4, 500, 520, 520), (2, 65, 264, 136), (6, 1000, 264, 520)])
+def test_two_graphs_of_one_workspace(B, N, E, F):
+    """Two captured backward passes share a workspace and are replayed in turn, with a call of the caller's own between them."""
+    mate = mate_module()
+    inputs = [Inputs(N + k, B, N, E, F, "tail") for k in range(2)]
+    kept = [mate.checkpoint_pack(i.x) for i in inputs]
+    ws = mate.linear_bwd_workspace(B, N, E, F, True, "cuda")
+    ws.fill_(255)
+
+    def step(k, space):
+        i = inputs[k]
+        return mate.linear_bwd(i.dy, kept[k], i.w, i.flags, z=i.z, act=mate.MATE_ACT_TANH, ws=space)
+
+    want = [step(k, None) for k in range(2)]
+    graphs, captured = [], []
+    for k in range(2):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=torch.cuda.Stream()):
+            captured.append(step(k, ws))
+        graphs.append(graph)
+    for replay in range(3):
+        for k in (0, 1, 1, 0):
+            for t in captured[k]:
+                t.fill_(77)
+            graphs[k].replay()
+            torch.cuda.synchronize()
+            assert all(torch.equal(u, v) for u, v in zip(captured[k], want[k])), (replay, k)
+            again = step(1 - k, ws)
+            torch.cuda.synchronize()
+            assert all(torch.equal(u, v) for u, v in zip(again, want[1 - k])), (replay, k)
+
+
+def test_few_tokens_in_a_graph_and_beside_each_other():
+    """Single tokens, as an answer's: replays in a graph, the same bits whichever tokens stand beside them in a call of the same sizes."""
+    mate = mate_module()
+    for B, N, E, F in ((1, 1, 768, 776), (3, 11, 264, 4096)):
+        i = Inputs(N, B, N, E, F, None)
+        kw = dict(act=mate.MATE_ACT_GELU, residual=i.res_y, keep_z=mate.MATE_KEEP_BF16)
+        want = mate.linear(i.x, i.w, i.bias, None, **kw)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=torch.cuda.Stream()):
+            got = mate.linear(i.x, i.w, i.bias, None, **kw)
+        for _ in range(3):
+            for t in got:
+                t.fill_(77)
+            graph.replay()
+            torch.cuda.synchronize()
+            assert all(torch.equal(u, v) for u, v in zip(got, want))
+        same = i.res_y.clone()
+        mate.linear(i.x, i.w, i.bias, None, act=mate.MATE_ACT_GELU, residual=same, y=same)
+        assert torch.equal(same, want[0])
+        x = i.x.clone()
+        x[:, 1:] = math.nan
+        y, z = mate.linear(x, i.w, i.bias, None, **kw)
+        assert torch.equal(y[:, 0], want[0][:, 0]) and torch.equal(z[:, 0], want[1][:, 0])
+        assert N == 1 or bool(torch.isnan(y[:, 1:]).all())
