@@ -6,10 +6,12 @@
 //              derivative p + z p (1 - p) (a + 3 b z^2)
 //   tanh       2 p(2 z) - 1, and below 1/16, where that cancels, z - z^3 / 3 + 2 z^5 / 15; derivative 4 p(2 |z|) (1 - p(2 |z|))
 //   gelu       z F(z), F the normal distribution function;  derivative F(z) + z f(z), f its density
-// F(-|z|) = 0.5 erfc(|z| / sqrt(2)) by formula 7.1.26 of Abramowitz and Stegun, t (a1 + .. + a5 t^4) e^(-z^2 / 2) with
-// t = 1 / (1 + 0.3275911 |z| / sqrt(2)), off by 1.5e-7 at most: no branch, one exponential, which the derivative's
-// density is as well, and an error that shrinks with e^(-z^2 / 2) in the tail instead of staying at an ulp of 1.
-// (A product's epilogue evaluates it for 67 million values of a large layer, 19 instruction slots each.)
+// gelu is max(z, 0) - |z| F(-|z|), and F(-t) = 2^p(t): its logarithm is smooth, so that a polynomial of degree 7 does (fitted here, for the
+// least largest error; relative to F it is below 2^-10 up to t = 9, and |z| F(-|z|) is off by 2.7e-7 at most, rounding included).  Beyond, p goes on
+// falling.  The derivative is S(-z) below 0 and 1 - S(z) above, S(t) = F(-t) - t f(t) = e^(-t^2 / 2) m(t), m a polynomial of degree 10 up
+// to t = 6.5, off by 4.4e-7 with rounding; beyond, where S is below 1e-8, m stays what it is there.  One exponential each and no quotient (a
+// hardware one takes as long as four additions): 14 and 21 instruction slots a value, where formula 7.1.26 of Abramowitz and Stegun
+// takes 20 and 24.
 #pragma once
 #include <hip/hip_runtime.h>
 
@@ -21,18 +23,33 @@ namespace mate {
 
 enum Activation { kActNone = 0, kActRelu = 1, kActGelu = 2, kActGeluTanh = 3, kActSilu = 4, kActTanh = 5 };
 
-__device__ __forceinline__ float logistic(float u) { return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-kLog2e * u)); }
+__device__ __forceinline__ float logistic_base2(float u) { return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(u)); }   // 1 / (1 + 2^u)
+__device__ __forceinline__ float logistic(float u) { return logistic_base2(-kLog2e * u); }
 
-// F(-|z|) and e^(-z^2 / 2)
-struct Normal { float tail, bell; };
-__device__ __forceinline__ Normal normal(float z) {
-  const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(0.3275911f * 0.70710678f, __builtin_fabsf(z), 1.f));
-  float s = __builtin_fmaf(t, 0.5f * 1.061405429f, 0.5f * -1.453152027f);
-  s = __builtin_fmaf(t, s, 0.5f * 1.421413741f);
-  s = __builtin_fmaf(t, s, 0.5f * -0.284496736f);
-  s = __builtin_fmaf(t, s, 0.5f * 0.254829592f);
-  const float bell = __builtin_amdgcn_exp2f(z * z * (-0.5f * kLog2e));
-  return {t * s * bell, bell};
+// F(-t), t >= 0
+__device__ __forceinline__ float normal_tail(float t) {
+  float p = __builtin_fmaf(t, -1.330662257714721e-06f, 5.147118281456642e-05f);
+  p = __builtin_fmaf(t, p, -0.000856266007758677f);
+  p = __builtin_fmaf(t, p, 0.008262364193797112f);
+  p = __builtin_fmaf(t, p, -0.05358245596289635f);
+  p = __builtin_fmaf(t, p, -0.45871248841285706f);
+  p = __builtin_fmaf(t, p, -1.1511999368667603f);
+  return __builtin_amdgcn_exp2f(__builtin_fmaf(t, p, -0.9999955296516418f));
+}
+// S(|z|); a NaN comes through the exponential.
+__device__ __forceinline__ float gelu_tail_slope(float z) {
+  const float t = __builtin_fminf(__builtin_fabsf(z), 6.5f);
+  float m = __builtin_fmaf(t, 7.85023814842134e-07f, -2.0947529264958575e-05f);
+  m = __builtin_fmaf(t, m, 0.00024150629178620875f);
+  m = __builtin_fmaf(t, m, -0.001614499487914145f);
+  m = __builtin_fmaf(t, m, 0.007173601072281599f);
+  m = __builtin_fmaf(t, m, -0.023348676040768623f);
+  m = __builtin_fmaf(t, m, 0.06044773757457733f);
+  m = __builtin_fmaf(t, m, -0.13223105669021606f);
+  m = __builtin_fmaf(t, m, 0.2498626410961151f);
+  m = __builtin_fmaf(t, m, -0.7978750467300415f);
+  m = __builtin_fmaf(t, m, 0.49999988079071045f);
+  return m * __builtin_amdgcn_exp2f(z * z * (-0.5f * kLog2e));
 }
 
 // Is z above 0, or not a number?  (A comparison alone would lose a NaN in relu.)
@@ -46,13 +63,15 @@ constexpr float kTanhSlope = 1.5957691216057308f, kTanhCubic = 0.044715f * kTanh
 template <int kAct>
 __device__ __forceinline__ float activate(float z) {
   if constexpr (kAct == kActRelu) return passes(z) ? z : 0.f;
-  // z F(z) = max(z, 0) - |z| F(-|z|).  (A NaN comes through F; where |z| is cut, F is zero, and infinity times zero would not be.)
-  if constexpr (kAct == kActGelu) return __builtin_fmaf(-__builtin_fminf(__builtin_fabsf(z), 64.f), normal(z).tail, __builtin_fmaxf(z, 0.f));
-  if constexpr (kAct == kActGeluTanh) return z * logistic(z * __builtin_fmaf(kTanhCubic, z * z, kTanhSlope));
+  // (A NaN comes through F; where |z| is cut, F is zero, and infinity times zero would not be.)
+  if constexpr (kAct == kActGelu) return __builtin_fmaf(-__builtin_fminf(__builtin_fabsf(z), 64.f), normal_tail(__builtin_fabsf(z)), __builtin_fmaxf(z, 0.f));
+  if constexpr (kAct == kActGeluTanh) return z * logistic_base2(z * __builtin_fmaf(-kLog2e * kTanhCubic, z * z, -kLog2e * kTanhSlope));
   if constexpr (kAct == kActSilu) return z * logistic(z);
   if constexpr (kAct == kActTanh) {
     const float z2 = z * z, small = __builtin_fmaf(z * z2, __builtin_fmaf(z2, 2.f / 15, -1.f / 3), z);
-    return __builtin_fabsf(z) < 0.0625f ? small : __builtin_fmaf(2.f, logistic(2.f * z), -1.f);
+    float large = __builtin_fmaf(2.f, logistic(2.f * z), -1.f);
+    asm volatile("" : "+v"(large));   // (computed for all: a branch around it, which the compiler would make, costs more)
+    return __builtin_fabsf(z) < 0.0625f ? small : large;
   }
   return z;
 }
@@ -63,11 +82,11 @@ __device__ __forceinline__ float slope(float z) {
   const float zc = __builtin_fminf(__builtin_fmaxf(z, -64.f), 64.f);
   if constexpr (kAct == kActRelu) return passes(z) ? 1.f : 0.f;
   if constexpr (kAct == kActGelu) {
-    const Normal n = normal(z);
-    return __builtin_fmaf(zc * 0.3989422804f, n.bell, z < 0.f ? n.tail : 1.f - n.tail);
+    const float s = gelu_tail_slope(z);
+    return z < 0.f ? s : 1.f - s;
   }
   if constexpr (kAct == kActGeluTanh || kAct == kActSilu) {
-    const float p = logistic(kAct == kActSilu ? z : z * __builtin_fmaf(kTanhCubic, z * z, kTanhSlope));
+    const float p = logistic_base2(z * (kAct == kActSilu ? -kLog2e : __builtin_fmaf(-kLog2e * kTanhCubic, z * z, -kLog2e * kTanhSlope)));
     const float inner = kAct == kActSilu ? zc : zc * __builtin_fmaf(3.f * kTanhCubic, zc * zc, kTanhSlope);
     return __builtin_fmaf(p * (1.f - p), inner, p);
   }

@@ -27,14 +27,15 @@ constexpr unsigned kLargestBits = 0x7f700000u;
 
 // A block's largest finite magnitude, as bits, which compare like it: of a lane's values, then across() the block's lanes.
 // Only if that is not finite, or close to the end of the range, are values looked at one by one (rare, so the common path has no test
-// per value); those above the largest are replaced by it.
+// per value); those above the largest are replaced by it.  (A comparison of numbers takes the sign off for nothing, and two values at a time.  One
+// with a NaN gives the other value, or the NaN, which is not finite.)
 __device__ __forceinline__ unsigned magnitude(float x) { return __float_as_uint(x) & 0x7fffffffu; }
 template <int kValues, class Across>
 __device__ __forceinline__ unsigned block_magnitude(float (&v)[kValues], Across&& across) {
-  unsigned m = 0;
+  float most = __builtin_fabsf(v[0]);
 #pragma unroll
-  for (int e = 0; e < kValues; ++e) m = max(m, magnitude(v[e]));
-  m = across(m);
+  for (int e = 1; e < kValues; ++e) most = __builtin_fmaxf(most, __builtin_fabsf(v[e]));
+  unsigned m = across(magnitude(most));
   if (__builtin_expect(__any(m > kLargestBits), 0)) {
     m = 0;
 #pragma unroll

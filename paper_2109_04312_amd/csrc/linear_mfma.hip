@@ -131,6 +131,8 @@ __device__ __forceinline__ void finish_as(const LinearStart& p, const LinearArgs
     return max(m, (unsigned)__builtin_amdgcn_update_dpp(0, (int)m, 0x4e, 0xf, 0xf, false));
   };
   const int from = token * kRow + ((c ^ token ^ (c >> 4)) << 4);
+  enum { kFarY = 1, kZ16 = 2, kZ8 = 4, kY8 = 8 };
+  const int results = __builtin_amdgcn_readfirstlane((a.far ? kFarY : 0) | (a.z ? a.z_scales ? kZ8 : kZ16 : 0) | (a.y_codes ? kY8 : 0));
   Read x[kAhead];
 #pragma unroll
   for (int k = 0; k < kAhead; ++k) x[k] = fetch(k);
@@ -195,13 +197,13 @@ __device__ __forceinline__ void finish_as(const LinearStart& p, const LinearArgs
           codes.store8<kNonTemporal>(at(step), to_codes(x[0], x[1], x[2], x[3], scale), to_codes(x[4], x[5], x[6], x[7], scale));
           scales_of.store1(lane & 3 ? kNowhere : scale_at(step), s);
         };
-        if (a.far) y.store16<kNonTemporal>(2 * at(step), words(v));
+        int wanted = results;
+        asm volatile("" : "+s"(wanted));   // (tested as a number: lane masks of what never changes would be kept, and made again in every step)
+        if (wanted & kFarY) y.store16<kNonTemporal>(2 * at(step), words(v));
         else y.store16(2 * at(step), words(v));
-        if (!kGrad && a.z) {
-          if (a.z_scales) store_8bit(z_out, z_scale, z);
-          else z_out.store16<kNonTemporal>(2 * at(step), words(z));
-        }
-        if (!kGrad && a.y_codes) store_8bit(y_code, y_scale, v);
+        if (!kGrad && (wanted & kZ16)) z_out.store16<kNonTemporal>(2 * at(step), words(z));
+        if (!kGrad && (wanted & kZ8)) store_8bit(z_out, z_scale, z);   // (last, as it may change z)
+        if (!kGrad && (wanted & kY8)) store_8bit(y_code, y_scale, v);
       }
     }
   }
