@@ -366,6 +366,8 @@ mate_status mate_out_project_bwd(const void* o, const void* w_o, const uint8_t* 
  *   y         [B, N, F] bf16
  *   z         NULL: not kept; z_scales NULL: [B, N, F] bf16; else codes, with z_scales
  *   y_codes, y_scales   y in 8 bits as well, for the backward of the product that reads y; or both NULL
+ *   workspace mate_linear_workspace_bytes(B, N, E, F, z_scales || y_codes) bytes (0: none is needed, as for most sizes: it
+ *             may be NULL then), at any address
  * z and y are rounded once, from fp32 (8 bits of either too: not from its bf16).  Rows of PAD tokens of every result are zeros.
  *
  * mate_linear_bwd:  with G = dy, its rows of PAD tokens counting as zero,
@@ -399,10 +401,11 @@ typedef enum {
   MATE_ACT_TANH = 5
 } mate_activation;
 enum { MATE_SCALE_BLOCK = 32 /* features that share a scale */, MATE_MAX_WIDTH = 65536 };
+size_t mate_linear_workspace_bytes(int B, int N, int E, int F, int in_codes);
 mate_status mate_linear(const void* x, const void* w, const float* bias, const uint8_t* flags,
                         const void* residual, int B, int N, int E, int F, mate_activation act,
                         mate_dtype t, void* y, void* z, uint8_t* z_scales, uint8_t* y_codes,
-                        uint8_t* y_scales, void* stream);
+                        uint8_t* y_scales, void* workspace, size_t workspace_bytes, void* stream);
 size_t mate_linear_bwd_workspace_bytes(int B, int N, int E, int F, int x_in_codes);
 mate_status mate_linear_bwd(const void* dy, const void* x, const uint8_t* x_scales, const void* w,
                             const uint8_t* flags, const void* z, const uint8_t* z_scales,

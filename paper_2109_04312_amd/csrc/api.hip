@@ -319,14 +319,21 @@ static_assert(MATE_ACT_NONE == kActNone && MATE_ACT_RELU == kActRelu && MATE_ACT
 mate_status done(hipError_t e) { return e == hipSuccess ? MATE_OK : MATE_ERR_HIP; }
 }  // namespace
 
+size_t mate_linear_workspace_bytes(int B, int N, int E, int F, int in_codes) {
+  if (!tokens_ok(B, N) || !width_ok(E) || !width_ok(F)) return 0;
+  return linear_workspace(B * N, E, F, in_codes != 0);
+}
+
 mate_status mate_linear(const void* x, const void* w, const float* bias, const uint8_t* flags,
                         const void* residual, int B, int N, int E, int F, mate_activation act,
                         mate_dtype t, void* y, void* z, uint8_t* z_scales, uint8_t* y_codes,
-                        uint8_t* y_scales, void* stream) {
+                        uint8_t* y_scales, void* workspace, size_t workspace_bytes, void* stream) {
   if (!x || !w || !y || (z_scales && !z) || !y_codes != !y_scales) return MATE_ERR_NULL;
   if (!tokens_ok(B, N) || E < 1 || F < 1) return MATE_ERR_SHAPE;
   if (t != MATE_BF16 || !width_ok(E) || !width_ok(F) || !act_ok(act) || !aligned({x, w, bias, residual, y, z, y_codes})) return MATE_ERR_UNSUPPORTED;
-  const LinearCall c = {x, w, bias, flags, residual, B * N, E, F, act, y, z, z_scales, y_codes, y_scales};
+  const size_t need = linear_workspace(B * N, E, F, z_scales || y_codes);
+  if (need && (!workspace || workspace_bytes < need)) return MATE_ERR_WORKSPACE;
+  const LinearCall c = {x, w, bias, flags, residual, B * N, E, F, act, y, z, z_scales, y_codes, y_scales, workspace, need ? next_ticket() : 0};
   return done(launch_linear(c, static_cast<hipStream_t>(stream)));
 }
 

@@ -33,8 +33,8 @@ namespace {
   X(mate_build_segments_bucketed) X(mate_cell_positions) X(mate_attn_fwd) X(mate_attn_bwd)        \
   X(mate_dense_workspace_bytes) X(mate_attn_fwd_dense) X(mate_attn_bwd_dense) X(mate_qkv_project) \
   X(mate_out_project) X(mate_project_bwd_workspace_bytes) X(mate_qkv_project_bwd)                 \
-  X(mate_out_project_bwd) X(mate_linear) X(mate_linear_bwd_workspace_bytes) X(mate_linear_bwd)                \
-  X(mate_activation_bwd) X(mate_checkpoint_pack) X(mate_checkpoint_unpack)
+  X(mate_out_project_bwd) X(mate_linear_workspace_bytes) X(mate_linear) X(mate_linear_bwd_workspace_bytes) \
+  X(mate_linear_bwd) X(mate_activation_bwd) X(mate_checkpoint_pack) X(mate_checkpoint_unpack)
 struct Abi {
 #define X(name) decltype(&::name) name;
   MATE_FUNCTIONS(X)
@@ -548,7 +548,7 @@ PyObject* tuple_of(std::initializer_list<PyObject*> items) {   // steals the ref
   return r;
 }
 
-PyObject* linear(Args a) {  // x, w, bias, flags, act, residual, keep_z, keep_y, y
+PyObject* linear(Args a) {  // x, w, bias, flags, act, residual, keep_z, keep_y, y, ws
   const at::Tensor &x = tensor(a[0], "x"), &w = tensor(a[1], "w");
   const Tokens s(x, "x");
   if (w.dim() != 2) fail(PyExc_ValueError, "w must have shape [F, E]");
@@ -572,10 +572,21 @@ PyObject* linear(Args a) {  // x, w, bias, flags, act, residual, keep_z, keep_y,
     pz = z8.code;
   }
   if (keep_y) y8 = Codes::fresh(d, s, F, x);
+  at::Tensor ws;
+  void* pws = nullptr;
+  size_t ws_bytes = 0;
+  if (a[9] != Py_None) {
+    ws = tensor(a[9], "ws");
+    pws = d.of(ws, at::kByte, ws.sizes(), "ws");
+    ws_bytes = (size_t)ws.numel();
+  } else if ((ws_bytes = abi.mate_linear_workspace_bytes(s.B, s.N, E, F, keep_z == 2 || keep_y))) {
+    ws = new_tensor({(int64_t)ws_bytes}, at::kByte, x);
+    pws = ws.data_ptr();
+  }
   void* st = d.stream();
   call("mate_linear", [&] {
     return abi.mate_linear(px, pw, (const float*)pb, (uint8_t*)pf, pr, s.B, s.N, E, F, (mate_activation)act, MATE_BF16, py, pz, z8.scale, y8.code,
-                           y8.scale, st);
+                           y8.scale, pws, ws_bytes, st);
   });
   PyObject* kept = z8 ? z8.wrap() : wrap_or_none(z);
   if (!keep_y) return tuple_of({THPVariable_Wrap(y), kept});
@@ -708,7 +719,7 @@ PyMethodDef methods[] = {METHOD(bind, 4),           METHOD(build_segments, 6),  
                          METHOD(cell_positions, 4), METHOD(attn_fwd, 9),        METHOD(attn_bwd, 13),
                          METHOD(attn_fwd_dense, 10), METHOD(attn_bwd_dense, 15), METHOD(qkv_project, 8),
                          METHOD(out_project, 5),    METHOD(qkv_project_bwd, 10), METHOD(out_project_bwd, 8),
-                         METHOD(linear, 9),         METHOD(linear_bwd, 11),     METHOD(activation_bwd, 5),   METHOD(checkpoint_pack, 3),
+                         METHOD(linear, 10),        METHOD(linear_bwd, 11),     METHOD(activation_bwd, 5),   METHOD(checkpoint_pack, 3),
                          METHOD(checkpoint_unpack, 3), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", "Tensor-level calls of the C ABI (see mate.py).", -1, methods};
 

@@ -134,8 +134,11 @@ struct LinearCall {
   int T, E, F, act;
   void *y, *z;
   unsigned char *z_scales, *y_codes, *y_scales;
+  void* workspace;
+  unsigned long long ticket;   // see arrival.h
 };
 hipError_t launch_linear(const LinearCall& c, hipStream_t stream);
+size_t linear_workspace(int T, int E, int F, bool codes);
 struct LinearBwdCall {
   const void *dy, *x;
   const unsigned char* x_scales;

@@ -291,8 +291,9 @@ __device__ __forceinline__ void contract_pipelined(const char* ring, int nk, con
   }
 }
 
-template <class S, bool kGrad>
-__device__ __forceinline__ void linear_tile(const LinearStart& p, const LinearArgs& a, char* lds, int t0, int f0) {
+// A tile, over the terms from stage `first` on, up to term k_end; merge(sums): whether this workgroup is the one that goes on with them.
+template <class S, bool kGrad, class Merge>
+__device__ __forceinline__ void linear_tile(const LinearStart& p, const LinearArgs& a, char* lds, int t0, int f0, int first, int k_end, Merge&& merge) {
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave_id = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int group = wave_id / S::kWaves, wave = wave_id - group * S::kWaves;
@@ -316,22 +317,22 @@ __device__ __forceinline__ void linear_tile(const LinearStart& p, const LinearAr
   const char* const w0 = reinterpret_cast<const char*>(kGrad ? p.w + f0 : p.w + (size_t)f0 * p.K);
   const char* const x0 = reinterpret_cast<const char*>(p.tok + (size_t)t0 * p.K);
   const size_t w_step = kGrad ? (size_t)64 * p.O * 2 : 128;
-  const char *w_ptr = w0 + group * w_step, *x_ptr = x0 + group * 128;   // of the next stage
-  const int stages = (p.K + 63) >> 6, nk = (stages + S::kGroups - 1) / S::kGroups;   // nk: this group's, the last one short or empty
-  const int short_k = 64 * ((nk - 1) * S::kGroups + group);   // its first term
-  const bool is_short = short_k + 64 > p.K;
+  const char *w_ptr = w0 + (first + group) * w_step, *x_ptr = x0 + (size_t)(first + group) * 128;   // of the next stage
+  const int stages = ((k_end + 63) >> 6) - first, nk = (stages + S::kGroups - 1) / S::kGroups;   // nk: this group's, the last one short or empty
+  const int short_k = 64 * (first + (nk - 1) * S::kGroups + group);   // its first term
+  const bool is_short = short_k + 64 > k_end;
   // Before a stage's loads: the short one's repeat the last 16 bytes, or rows (no other stage follows).
   auto prepare_stage = [&](int g) {
     if (__builtin_expect(g == nk - 1 && is_short, 0)) {
-      const int row0 = min(short_k, p.K - 1);
+      const int row0 = min(short_k, k_end - 1);
       w_ptr = kGrad ? w0 + (size_t)row0 * p.O * 2 : w0;
       x_ptr = x0;
 #pragma unroll
       for (int i = 0; i < S::kLoads; ++i) {
         const bool is_a = i < S::kLoadsA;
         const LoadUnit l = load_unit<S::kWaves>(wave, lane, is_a ? i : i - S::kLoadsA);
-        if (kGrad && is_a) off[i] -= (unsigned)(l.row - (min(short_k + l.row, p.K - 1) - row0)) * (unsigned)p.O * 2;
-        else off[i] += (unsigned)min(short_k + 8 * l.chunk, p.K - 8) * 2 - l.chunk * 16;
+        if (kGrad && is_a) off[i] -= (unsigned)(l.row - (min(short_k + l.row, k_end - 1) - row0)) * (unsigned)p.O * 2;
+        else off[i] += (unsigned)min(short_k + 8 * l.chunk, k_end - 8) * 2 - l.chunk * 16;
       }
     }
   };
@@ -358,7 +359,7 @@ __device__ __forceinline__ void linear_tile(const LinearStart& p, const LinearAr
       const bool is_a = i < S::kLoadsA;
       const int y = is_a ? i : i - S::kLoadsA;
       const LoadUnit l = load_unit<S::kWaves>(wave, lane, y);
-      if (short_k + (kGrad && is_a ? l.row : 8 * l.chunk) >= p.K)
+      if (short_k + (kGrad && is_a ? l.row : 8 * l.chunk) >= k_end)
         *reinterpret_cast<uint4*>(st + (is_a ? 0 : S::kA * kTileBytes) + load_dst<S::kWaves>(wave, y) + lane * 16) = make_uint4(0, 0, 0, 0);
     }
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
@@ -406,11 +407,17 @@ __device__ __forceinline__ void linear_tile(const LinearStart& p, const LinearAr
   }
   f32x4 sum[S::kFA][S::kOutB];
   add_groups<S>(acc, sum, lds, group, wave, lane);
+  if (!merge(sum, wave_id)) return;
 
   constexpr int kWaveArea = S::kLds / S::kAllWaves / 1024 * 1024, kFit = std::min(S::kOutB, kWaveArea / (S::kFA * 1024));
   constexpr int kArea = S::kOutB % kFit == 0 ? kFit : kFit - 1;
   __syncthreads();   // (everyone is done with the stages)
   finish<S::kFA, S::kOutB, kArea, kGrad>(p, a, sum, lds + wave_id * kWaveArea, t0 + (wb * S::kFB + group * S::kOutB) * 16, f0 + wa * S::kFA * 16);
+}
+
+template <class S, bool kGrad>
+__device__ __forceinline__ void linear_tile(const LinearStart& p, const LinearArgs& a, char* lds, int t0, int f0) {
+  linear_tile<S, kGrad>(p, a, lds, t0, f0, 0, p.K, [](f32x4 (&)[S::kFA][S::kOutB], int) { return true; });
 }
 
 template <class S, bool kGrad>
@@ -453,6 +460,37 @@ hipError_t launch_product(LinearArgs a, hipStream_t stream) {
   if (e != hipSuccess) return e;
   hipLaunchKernelGGL((linear_kernel<S, kGrad>), grid, dim3(S::kThreads), S::kLds, stream, a.w, a.tok, a.T, a.O, a.K, d.tokens, d.features, d.rows,
                      d.by_feature, a);
+  return hipGetLastError();
+}
+
+// Few tiles of a long contraction: each is shared by the workgroups of several ranges of it, whose sums the launch adds.  Ranges of all
+// tiles follow each other, so that every XCD has the same tiles in each.
+template <class S>
+__global__ __launch_bounds__(S::kThreads, S::kAllWaves / 4 * S::kPerCU) void linear_split_kernel(const unsigned short* w, const unsigned short* tok, int T,
+                                                                                               int O, int K, int token_tiles, int feature_tiles,
+                                                                                               int whole_rows, int by_feature, RangeMerge m, LinearArgs a) {
+  extern __shared__ __attribute__((aligned(1024))) char lds[];
+  const LinearStart p = {w, tok, T, O, K, {token_tiles, feature_tiles, whole_rows, by_feature}};
+  int y, token_tile, feature_tile;
+  const int range = uniform_div(blockIdx.y, p.deal.grid_y(), y), stages = (K + 63) >> 6;
+  if (!dealt_tile(p.deal, blockIdx.x, y, token_tile, feature_tile)) return;
+  linear_tile<S, false>(p, a, lds, token_tile * S::kRowsB, feature_tile * S::kRowsA, stages * range / m.splits, min(K, 64 * (stages * (range + 1) / m.splits)),
+                        [&](f32x4 (&sum)[S::kFA][S::kOutB], int wave_id) {
+                          float none[S::kFB] = {};
+                          return merge_ranges<S>(m, range, token_tile * feature_tiles + feature_tile, 0, false, sum, none, wave_id);
+                        });
+}
+template <class S>
+hipError_t launch_split(LinearArgs a, int splits, void* workspace, unsigned long long ticket, hipStream_t stream) {
+  deal_tiles<S>(a);
+  const TileDeal& d = a.deal;
+  const int tiles = d.tokens * d.features;
+  RangeMerge m = {static_cast<float*>(workspace), nullptr, nullptr, ticket, splits, tiles, 0};
+  m.arrived = reinterpret_cast<unsigned long long*>(m.part + (size_t)splits * tiles * S::kRowsA * S::kRowsB);
+  const hipError_t e = allow_lds<&linear_split_kernel<S>>(S::kLds);
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL((linear_split_kernel<S>), dim3(d.grid_x(), d.grid_y() * splits), dim3(S::kThreads), S::kLds, stream, a.w, a.tok, a.T, a.O, a.K,
+                     d.tokens, d.features, d.rows, d.by_feature, m, a);
   return hipGetLastError();
 }
 
@@ -616,6 +654,43 @@ FewChoice choose_few(int T, int O, int K) {
                              few_as<16, 1, 4>(T, O, K), few_as<16, 2, 2>(T, O, K), few_as<16, 2, 4>(T, O, K)})
     if (c.cost < best.cost) best = c;
   return best;
+}
+
+// A split contraction: in ranges of 16 stages or more, at most one workgroup a unit.  Tiles of 64 tokens only: with those of 128 both the ranges and
+// their addition take longer (1000 tokens 4096 -> 768, halves: 21.1 us, by 64 16.4), and where only they leave units without a tile, they gain
+// nothing (1999 tokens 4096 -> 1024 24.8 whole, 25.3 in halves).  us, as above and split: 512 tokens 4096 -> 768 24.2 and 16.4, 2048 -> 768 13.8 and
+// 11.4, 1000 tokens 4096 -> 256 17.1 and 13.5, -> 1024 22.0 and 17.5, 300 tokens 2048 -> 1024 13.4 and 11.3; 1024 long, halves would be no faster.
+struct SplitChoice {
+  double cost;
+  int splits;
+  size_t bytes;
+};
+using TileSplit = Tile64x2;
+SplitChoice choose_split(int T, int O, int K) {
+  SplitChoice best = {1e30, 0, 0};
+  const size_t tiles = (T + (size_t)TileSplit::kRowsB - 1) / TileSplit::kRowsB * ((O + TileSplit::kRowsA - 1) / TileSplit::kRowsA);
+  const int stages = (K + 63) / 64;
+  for (int splits = 2; splits <= kMaxRanges && tiles * splits <= 256 && stages >= 16 * splits; ++splits) {
+    double cost = (stages + splits - 1) / splits * 0.29 + 0.9;
+    for (int r = 1; r < splits; r *= 2) cost += 2.6 + 0.6 * (double)(tiles * splits) / 256;   // one addition of pairs
+    if (cost < best.cost) best = {cost, splits, tiles * (splits * (size_t)(TileSplit::kRowsA * TileSplit::kRowsB * 4) + kMaxRanges * 8)};
+  }
+  return best;
+}
+
+// How a forward product is computed, by its sizes (and whether results in 8 bits are wanted, which few tokens' kernels do not give).
+struct ForwardPlan {
+  ProductChoice tiles;
+  FewChoice few;      // if its launch is not null
+  SplitChoice split;  // or if its splits are not 0
+};
+ForwardPlan plan_forward(int T, int O, int K, bool codes) {
+  ForwardPlan p = {choose_product<false>(T, O, K), {1e30, nullptr}, choose_split(T, O, K)};
+  if (p.split.cost >= p.tiles.cost) p.split = {p.tiles.cost, 0, 0};
+  if (T <= kFewTokens && !codes) p.few = choose_few(T, O, K);
+  if (p.few.cost < p.split.cost + 3.0) p.split.splits = 0;
+  else p.few.launch = nullptr;
+  return p;
 }
 
 // ======================================================================================
@@ -1028,12 +1103,15 @@ hipError_t launch_linear(const LinearCall& c, hipStream_t stream) {
   a.z_scales = c.z_scales;
   a.y_codes = c.y_codes;
   a.y_scales = c.y_scales;
-  const ProductChoice tiles = choose_product<false>(a.T, a.O, a.K);
-  if (a.T <= kFewTokens && !a.z_scales && !a.y_codes) {
-    const FewChoice few = choose_few(a.T, a.O, a.K);
-    if (few.cost < tiles.cost + 3.0) return few.launch(a, stream);
-  }
-  return tiles.launch(a, stream);
+  const ForwardPlan p = plan_forward(a.T, a.O, a.K, a.z_scales || a.y_codes);
+  if (p.few.launch) return p.few.launch(a, stream);
+  if (!p.split.splits) return p.tiles.launch(a, stream);
+  char* ws = static_cast<char*>(c.workspace);
+  return launch_split<TileSplit>(a, p.split.splits, ws + (-reinterpret_cast<uintptr_t>(ws) & 15), c.ticket, stream);
+}
+size_t linear_workspace(int T, int E, int F, bool codes) {
+  const ForwardPlan p = plan_forward(T, F, E, codes);
+  return p.split.splits ? p.split.bytes + 16 : 0;   // (the caller's address may be any)
 }
 
 size_t linear_bwd_workspace(int T, int E, int F, bool codes) { return plan_backward(T, E, F, codes).total; }   // (the caller's address may be any)

@@ -29,7 +29,7 @@ MATE_MAX_N, MATE_MAX_HEADS, MATE_HEAD_DIM = 16384, 256, 64
 EXPORTS = ["mate_segments_bytes", "mate_workspace_bytes", "mate_build_segments",
            "mate_build_segments_bucketed", "mate_cell_positions", "mate_segments_export", "mate_segments_export_windows", "mate_attn_fwd", "mate_attn_bwd", "mate_dense_workspace_bytes",
            "mate_attn_fwd_dense", "mate_attn_bwd_dense", "mate_attn_bwd_dense_static", "mate_attn_prefers_dense", "mate_segments_status", "mate_qkv_project", "mate_out_project", "mate_project_bwd_workspace_bytes", "mate_qkv_project_bwd", "mate_out_project_bwd",
-           "mate_linear", "mate_linear_bwd_workspace_bytes", "mate_linear_bwd", "mate_activation_bwd", "mate_checkpoint_pack", "mate_checkpoint_unpack", "mate_profile_kernel",
+           "mate_linear_workspace_bytes", "mate_linear", "mate_linear_bwd_workspace_bytes", "mate_linear_bwd", "mate_activation_bwd", "mate_checkpoint_pack", "mate_checkpoint_unpack", "mate_profile_kernel",
            "mate_probe_mfma", "mate_status_string"]
 MATE_KERNEL_NONE, MATE_KERNEL_BUILD, MATE_KERNEL_FWD = 0, 1, 2
 MATE_KERNEL_BWD_DQ, MATE_KERNEL_BWD_DKV = 3, 4
@@ -96,8 +96,10 @@ _lib.mate_qkv_project_bwd.restype = _i
 _lib.mate_qkv_project_bwd.argtypes = [_p, _p, _p, _p, _p, _p, _i, _i, _i, _i, _i, _p, _p, _p, _p, _sz, _p]
 _lib.mate_out_project_bwd.restype = _i
 _lib.mate_out_project_bwd.argtypes = [_p, _p, _p, _p, _i, _i, _i, _i, _i, _p, _p, _p, _p, _sz, _p]
+_lib.mate_linear_workspace_bytes.restype = _sz
+_lib.mate_linear_workspace_bytes.argtypes = [_i, _i, _i, _i, _i]
 _lib.mate_linear.restype = _i
-_lib.mate_linear.argtypes = [_p, _p, _p, _p, _p, _i, _i, _i, _i, _i, _i, _p, _p, _p, _p, _p, _p]
+_lib.mate_linear.argtypes = [_p, _p, _p, _p, _p, _i, _i, _i, _i, _i, _i, _p, _p, _p, _p, _p, _p, _sz, _p]
 _lib.mate_linear_bwd_workspace_bytes.restype = _sz
 _lib.mate_linear_bwd_workspace_bytes.argtypes = [_i, _i, _i, _i, _i]
 _lib.mate_linear_bwd.restype = _i
@@ -138,6 +140,7 @@ mate_out_project = _lib.mate_out_project
 mate_project_bwd_workspace_bytes = _lib.mate_project_bwd_workspace_bytes
 mate_qkv_project_bwd = _lib.mate_qkv_project_bwd
 mate_out_project_bwd = _lib.mate_out_project_bwd
+mate_linear_workspace_bytes = _lib.mate_linear_workspace_bytes
 mate_linear = _lib.mate_linear
 mate_linear_bwd_workspace_bytes = _lib.mate_linear_bwd_workspace_bytes
 mate_linear_bwd = _lib.mate_linear_bwd
@@ -274,11 +277,16 @@ def out_project_bwd(o, w_o, flags, dy, want_do=True, want_dw=True, want_dbias=Tr
     return _native.out_project_bwd(o, w_o, flags, dy, want_do, want_dw, want_dbias, ws)
 
 
-def linear(x, w, bias=None, flags=None, act=MATE_ACT_NONE, residual=None, keep_z=MATE_KEEP_NONE, keep_y=False, y=None):
+def linear_workspace(B, N, E, F, in_codes, device) -> torch.Tensor:
+    """What linear() needs beside its results (often nothing); in_codes: does it keep z or y in 8 bits?"""
+    return torch.empty(mate_linear_workspace_bytes(B, N, E, F, int(in_codes)), dtype=torch.uint8, device=device)
+
+
+def linear(x, w, bias=None, flags=None, act=MATE_ACT_NONE, residual=None, keep_z=MATE_KEEP_NONE, keep_y=False, y=None, ws=None):
     """z = x w^T + bias, y = act(z) + residual: x [B,N,E] bf16, w [F,E] bf16, bias [F] float32 or None, residual [B,N,F] bf16
     or None (it may be y) -> (y [B,N,F] bf16, z), z for the backward as keep_z says: None, bf16 or a Checkpoint.  keep_y: a third
     result, y as a Checkpoint, for the backward of the product that reads y."""
-    return _native.linear(x, w, bias, flags, act, residual, keep_z, keep_y, y)
+    return _native.linear(x, w, bias, flags, act, residual, keep_z, keep_y, y, ws)
 
 
 def linear_bwd_workspace(B, N, E, F, x_in_codes, device) -> torch.Tensor:

@@ -15,8 +15,8 @@ def refuses(f, ok, cases):
 
 
 def test_linear():
-    #    x, w, bias, flags, residual, B, N, E, F, act, t, y, z, z_scales, y_codes, y_scales, stream
-    ok = [FAKE, FAKE, FAKE, FAKE, FAKE, 2, 100, 768, 1000, mate.MATE_ACT_GELU, mate.MATE_BF16, FAKE, FAKE, FAKE, FAKE, FAKE, None]
+    #    x, w, bias, flags, residual, B, N, E, F, act, t, y, z, z_scales, y_codes, y_scales, ws, bytes, stream
+    ok = [FAKE, FAKE, FAKE, FAKE, FAKE, 2, 100, 768, 1000, mate.MATE_ACT_GELU, mate.MATE_BF16, FAKE, FAKE, FAKE, FAKE, FAKE, None, 0, None]
     refuses(mate.mate_linear, ok, [
         (0, None, mate.MATE_ERR_NULL), (1, None, mate.MATE_ERR_NULL), (11, None, mate.MATE_ERR_NULL), (12, None, mate.MATE_ERR_NULL),
         (14, None, mate.MATE_ERR_NULL), (15, None, mate.MATE_ERR_NULL),
@@ -25,6 +25,12 @@ def test_linear():
         (7, 764, mate.MATE_ERR_UNSUPPORTED), (8, 1001, mate.MATE_ERR_UNSUPPORTED), (7, mate.MATE_MAX_WIDTH + 8, mate.MATE_ERR_UNSUPPORTED),
         (9, 6, mate.MATE_ERR_UNSUPPORTED), (9, -1, mate.MATE_ERR_UNSUPPORTED), (10, mate.MATE_F32, mate.MATE_ERR_UNSUPPORTED),
         *((i, FAKE + 8, mate.MATE_ERR_UNSUPPORTED) for i in (0, 1, 2, 4, 11, 12, 14))])
+    assert mate.mate_linear_workspace_bytes(2, 100, 768, 1000, 1) == 0       # none is needed
+    assert mate.mate_linear_workspace_bytes(2, 0, 768, 1000, 1) == mate.mate_linear_workspace_bytes(2, 100, 764, 1000, 1) == 0
+    need = mate.mate_linear_workspace_bytes(1, 300, 4096, 1000, 1)           # few tiles of a long contraction
+    assert need > 0
+    ok[5:9], ok[16:18] = [1, 300, 4096, 1000], [FAKE, need]
+    refuses(mate.mate_linear, ok, [(16, None, mate.MATE_ERR_WORKSPACE), (17, need - 1, mate.MATE_ERR_WORKSPACE)])
 
 
 def test_linear_bwd():

@@ -612,3 +612,66 @@ def test_few_tokens_in_a_graph_and_beside_each_other():
         y, z = mate.linear(x, i.w, i.bias, None, **kw)
         assert torch.equal(y[:, 0], want[0][:, 0]) and torch.equal(z[:, 0], want[1][:, 0])
         assert N == 1 or bool(torch.isnan(y[:, 1:]).all())
+
+
+# a contraction shared by two, three and four ranges, with a rest for the last one, tiles that are not full, one that is padding
+SPLITS = [(1, 300, 2048, 1024), (2, 500, 4096, 264), (3, 100, 4104, 776), (1, 515, 4032, 1032), (5, 400, 1992, 136), (1, 64, 4096, 8)]
+
+
+@pytest.mark.parametrize("B,N,E,F", SPLITS)
+def test_split_contractions(B, N, E, F):
+    check_forward(N, B, N, E, F, "gelu", padding="scattered")
+    check_forward(N + 1, B, N, E, F, "none", bias=False, residual=False, keep_z=1, keep_y=False)
+    check_forward(N + 2, B, N, E, F, "silu", padding="all")
+
+
+def test_split_contractions_again_together_and_in_graphs():
+    """The same bits in every run: on two streams at once, and from two graphs that share a workspace, full of NaN at first and at an odd address."""
+    mate = mate_module()
+    B, N, E, F = 3, 100, 4104, 776
+    inputs = [Inputs(k, B, N, E, F, "scattered") for k in range(2)]
+    size = mate.mate_linear_workspace_bytes(B, N, E, F, 1)
+    assert size > 0
+
+    def step(k, ws=None):
+        i = inputs[k]
+        y, z = mate.linear(i.x, i.w, i.bias, i.flags, act=mate.MATE_ACT_GELU, residual=i.res_y, keep_z=mate.MATE_KEEP_8BIT, ws=ws)
+        return y, z.codes, z.scales
+
+    want = [step(k) for k in range(2)]
+    room = [torch.full((size + 5,), 255, dtype=torch.uint8, device="cuda") for k in range(2)]
+    ws = [t[5:] for t in room]
+    torch.cuda.synchronize()
+    streams, got = [torch.cuda.Stream(), torch.cuda.Stream()], []
+    for _ in range(5):
+        for k in range(2):
+            with torch.cuda.stream(streams[k]):
+                got.append((k, step(k, ws[k])))
+    torch.cuda.synchronize()
+    for k, g in got:
+        assert all(torch.equal(u, v) for u, v in zip(g, want[k]))
+    graphs, captured = [], []
+    for k in range(2):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=torch.cuda.Stream()):
+            captured.append(step(k, ws[0]))
+        graphs.append(graph)
+    for replay in range(3):
+        for k in (0, 1, 1, 0):
+            for t in captured[k]:
+                t.fill_(77)
+            graphs[k].replay()
+            torch.cuda.synchronize()
+            assert all(torch.equal(u, v) for u, v in zip(captured[k], want[k])), (replay, k)
+            assert all(torch.equal(u, v) for u, v in zip(step(1 - k, ws[0]), want[1 - k])), (replay, k)
+    with pytest.raises(mate.MateError) as e:
+        step(0, ws[0][:size - 1])
+    assert e.value.status == mate.MATE_ERR_WORKSPACE
+    i = inputs[0]
+    x = i.x.clone()
+    x[0, 3, -1] = math.nan                        # of the last range
+    x[0, 5, 0] = math.inf                         # of the first
+    y, z = mate.linear(x, i.w, i.bias, None, keep_z=mate.MATE_KEEP_8BIT)
+    sick = torch.zeros(B, N, dtype=torch.bool, device="cuda")
+    sick[0, 3] = sick[0, 5] = True
+    assert torch.equal(torch.isfinite(y).all(-1), ~sick) and torch.equal(torch.isnan(mate.checkpoint_unpack(z)).any(-1), sick)
