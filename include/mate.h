@@ -368,7 +368,8 @@ mate_status mate_out_project_bwd(const void* o, const void* w_o, const uint8_t* 
  *   y_codes, y_scales   y in 8 bits as well, for the backward of the product that reads y; or both NULL
  *   workspace mate_linear_workspace_bytes(B, N, E, F, z_scales || y_codes) bytes (0: none is needed, as for most sizes: it
  *             may be NULL then), at any address
- * z and y are rounded once, from fp32 (8 bits of either too: not from its bf16).  Rows of PAD tokens of every result are zeros.
+ * z and y are rounded once, from fp32 (8 bits of either too: not from its bf16).  Rows of PAD tokens of every result are zeros,
+ * whatever x and residual hold there; infinities and NaN elsewhere reach the results of their token only.
  *
  * mate_linear_bwd:  with G = dy, its rows of PAD tokens counting as zero,
  *     dx    = (G w) * act'(z) + residual    [B, N, E] bf16, rows of PAD tokens written 0
@@ -382,6 +383,7 @@ mate_status mate_out_project_bwd(const void* o, const void* w_o, const uint8_t* 
  *   dx, dw, dbias   any may be NULL (not computed); dbias needs dw
  *   workspace mate_linear_bwd_workspace_bytes(B, N, E, F, x_scales != NULL) bytes (0: sizes out of range), at any address;
  *             needed for dw only
+ * As ever, calls that may run at the same time need workspaces of their own; one after the other they may share one, captured ones too.
  * A layer y = act(x w^T + b) whose next product is y w2^T: mate_linear_bwd of the second with z and act of the first gives the
  * gradient at z, which is dy of the first one's mate_linear_bwd.  The result does not depend on whether the other gradient is wanted.
  *
@@ -429,9 +431,9 @@ mate_status mate_checkpoint_unpack(const uint8_t* codes, const uint8_t* scales, 
  * created with timing enabled and owned by the caller.  kernel = MATE_KERNEL_NONE disarms.
  * Up to 256 positions the backward of the dense-mask variant is one launch, and so are the bf16 backward (behind
  * a short one) where B * H * ceil(N / 128) is small (at most 768) and both gradients of a projection of a small layer; both names mean
- * that one then.  The kernels of MATE_F32 have no name.
+ * that one then.  The kernels of MATE_F32 have no name, nor do those of the feed-forward half.
  * The hook is per host thread.  The library keeps no other state that a caller can see: besides it a
- * counter that numbers the forward and projection backward calls of the process, the static array of
+ * counter that numbers the calls of the process whose workgroups leave sums for each other, the static array of
  * mate_attn_bwd_dense_static, and launch settings per device.
  */
 enum { MATE_KERNEL_NONE = 0, MATE_KERNEL_BUILD = 1, MATE_KERNEL_FWD = 2, MATE_KERNEL_BWD_DQ = 3,
