@@ -392,7 +392,8 @@ mate_status mate_out_project_bwd(const void* o, const void* w_o, const uint8_t* 
  *
  * mate_checkpoint_pack: x -> codes, scales;  mate_checkpoint_unpack: codes, scales -> x.  x: [B, N, E] of dtype t, MATE_BF16 or MATE_F32.
  *
- * fp32 accumulation throughout.  Asynchronous on `stream`; deterministic.
+ * fp32 accumulation throughout.  Asynchronous on `stream`; deterministic: the same call has the same bits.  (The order of a sum goes by the sizes
+ * and, in mate_linear, by whether z or y is kept in 8 bits.)
  */
 typedef enum {
   MATE_ACT_NONE = 0,

@@ -120,10 +120,7 @@ __global__ __launch_bounds__(kThreads) void pack_kernel(const void* x, const uns
         load_values<kF32>(x, d, u, v[k]);
       },
       [&](int k, const Unit& u) {
-        const unsigned s = scale_byte(block_magnitude(v[k], [](unsigned m) {
-          m = max(m, (unsigned)__builtin_amdgcn_update_dpp(0, (int)m, 0xb1, 0xf, 0xf, false));
-          return max(m, (unsigned)__builtin_amdgcn_update_dpp(0, (int)m, 0x4e, 0xf, 0xf, false));
-        }));
+        const unsigned s = scale_byte(block_magnitude(v[k], quad_maximum));
         if (!u.some) return;
         const float scale = scale_value(s);
         *reinterpret_cast<uint2*>(codes + u.row * d.E + u.first) =

@@ -50,6 +50,11 @@ __device__ __forceinline__ unsigned block_magnitude(float (&v)[kValues], Across&
   }
   return m;
 }
+// Across the four lanes of a quad.
+__device__ __forceinline__ unsigned quad_maximum(unsigned m) {
+  m = max(m, (unsigned)__builtin_amdgcn_update_dpp(0, (int)m, 0xb1, 0xf, 0xf, false));
+  return max(m, (unsigned)__builtin_amdgcn_update_dpp(0, (int)m, 0x4e, 0xf, 0xf, false));
+}
 // The scale's byte for the bits of a block's largest magnitude: its exponent less 8, one more above 1.75.
 __device__ __forceinline__ unsigned scale_byte(unsigned magnitude_bits) {
   const int s = (int)((magnitude_bits + 0x1fffffu) >> 23) - 8;

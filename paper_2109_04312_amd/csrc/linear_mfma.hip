@@ -126,10 +126,6 @@ __device__ __forceinline__ void finish_as(const LinearStart& p, const LinearArgs
     }
     return x;
   };
-  auto quad_magnitude = [](unsigned m) {
-    m = max(m, (unsigned)__builtin_amdgcn_update_dpp(0, (int)m, 0xb1, 0xf, 0xf, false));
-    return max(m, (unsigned)__builtin_amdgcn_update_dpp(0, (int)m, 0x4e, 0xf, 0xf, false));
-  };
   const int from = token * kRow + ((c ^ token ^ (c >> 4)) << 4);
   enum { kFarY = 1, kZ16 = 2, kZ8 = 4, kY8 = 8 };
   const int results = __builtin_amdgcn_readfirstlane((a.far ? kFarY : 0) | (a.z ? a.z_scales ? kZ8 : kZ16 : 0) | (a.y_codes ? kY8 : 0));
@@ -192,7 +188,7 @@ __device__ __forceinline__ void finish_as(const LinearStart& p, const LinearArgs
         x[k] = fetch(step + kAhead);   // (past the last step: zeros)
         auto words = [](const float (&x)[8]) { return u32x4{pack2(x[0], x[1]), pack2(x[2], x[3]), pack2(x[4], x[5]), pack2(x[6], x[7])}; };
         auto store_8bit = [&](const Part& codes, const Part& scales_of, float (&x)[8]) {
-          const unsigned s = scale_byte(block_magnitude(x, quad_magnitude));
+          const unsigned s = scale_byte(block_magnitude(x, quad_maximum));
           const float scale = scale_value(s);
           codes.store8<kNonTemporal>(at(step), to_codes(x[0], x[1], x[2], x[3], scale), to_codes(x[4], x[5], x[6], x[7], scale));
           scales_of.store1(lane & 3 ? kNowhere : scale_at(step), s);
@@ -603,29 +599,63 @@ __global__ __launch_bounds__(512) void few_kernel(const unsigned short* w, const
       part[wave][i * kFB + j][lane] = x;
     }
   __syncthreads();
-  if (wave >= kBlocks) return;
-  f32x4 z = part[0][wave][lane];
+  const bool codes = kFA == 2 && (a.z_scales || a.y_codes);
+  if (wave >= kBlocks && !codes) return;
+  f32x4 z = {0.f, 0.f, 0.f, 0.f}, y = z;
+  if (wave < kBlocks) {
+    z = part[0][wave][lane];
 #pragma unroll
-  for (int v = 1; v < kWaves; ++v) z += part[v][wave][lane];
-  if (kParts > 1)
+    for (int v = 1; v < kWaves; ++v) z += part[v][wave][lane];
+    if (kParts > 1)
 #pragma unroll
-    for (int e = 0; e < 4; ++e) z[e] = kParts == 4 ? quad_sum(z[e]) : half_sum(z[e]);
-  const int i = wave / kFB, t = t0 + 16 * (wave - i * kFB) + r, f = f0 + 16 * i + 4 * q;   // a lane's four features of a token
-  if (t >= T || f >= O || 4 * q >= kRows) return;
-  const size_t at = (size_t)t * O + f;
-  uint2 add = make_uint2(0, 0);
-  if (a.add) add = *reinterpret_cast<const uint2*>(a.add + at);
-  if (a.bias) z += *reinterpret_cast<const f32x4*>(a.bias + f);
-  const bool pad = a.flags && a.flags[t] >= 2;
-  f32x4 y = z;
-  with_activation(a.act, [&](auto kind) {
+      for (int e = 0; e < 4; ++e) z[e] = kParts == 4 ? quad_sum(z[e]) : half_sum(z[e]);
+    const int i = wave / kFB, t = t0 + 16 * (wave - i * kFB) + r, f = f0 + 16 * i + 4 * q;   // a lane's four features of a token
+    const bool real = t < T && f < O && 4 * q < kRows;
+    if (!codes && !real) return;
+    const size_t at = (size_t)t * O + f;
+    uint2 add = make_uint2(0, 0);
+    if (a.add && real) add = *reinterpret_cast<const uint2*>(a.add + at);
+    if (a.bias && real) z += *reinterpret_cast<const f32x4*>(a.bias + f);
+    const bool pad = !real || (a.flags && a.flags[t] >= 2);
+    with_activation(a.act, [&](auto kind) {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) y[e] = activate<decltype(kind)::value>(z[e]);
-  });
-  if (a.add) y += f32x4{low_bf16(add.x), high_bf16(add.x), low_bf16(add.y), high_bf16(add.y)};
-  if (pad) y = z = f32x4{0.f, 0.f, 0.f, 0.f};
-  if (a.z) *reinterpret_cast<uint2*>(static_cast<unsigned short*>(a.z) + at) = make_uint2(pack2(z[0], z[1]), pack2(z[2], z[3]));
-  *reinterpret_cast<uint2*>(a.y + at) = make_uint2(pack2(y[0], y[1]), pack2(y[2], y[3]));
+      for (int e = 0; e < 4; ++e) y[e] = activate<decltype(kind)::value>(z[e]);
+    });
+    if (a.add) y += f32x4{low_bf16(add.x), high_bf16(add.x), low_bf16(add.y), high_bf16(add.y)};
+    if (pad) y = z = f32x4{0.f, 0.f, 0.f, 0.f};
+    if (real) {
+      if (a.z && !a.z_scales) *reinterpret_cast<uint2*>(static_cast<unsigned short*>(a.z) + at) = make_uint2(pack2(z[0], z[1]), pack2(z[2], z[3]));
+      *reinterpret_cast<uint2*>(a.y + at) = make_uint2(pack2(y[0], y[1]), pack2(y[2], y[3]));
+    }
+  }
+  if constexpr (kFA == 2) {
+    // 8 bits: the workgroup's 32 features of a token have one scale.  Through LDS, so that four lanes have a token, eight features each.
+    if (!codes) return;
+    constexpr int kTokens = 16 * kFB;
+    static_assert(2 * kTokens * 32 * sizeof(float) <= sizeof(part) && 4 * kTokens <= 512, "room for both, and a thread for eight values");
+    f32x4* const staged = &part[0][0][0];   // [z, y][token][four features]
+    __syncthreads();                        // (the sums have been read)
+    if (wave < kBlocks) {
+      const int i = wave / kFB, to = (16 * (wave - i * kFB) + r) * 8 + 4 * i + q;
+      staged[to] = z;
+      staged[kTokens * 8 + to] = y;
+    }
+    __syncthreads();
+    if ((int)threadIdx.x >= 4 * kTokens) return;
+    const int token = threadIdx.x >> 2, t = t0 + token, f = f0 + 8 * (threadIdx.x & 3), scales = scale_blocks(O);
+    const bool real = t < T && f < O;
+    auto keep = [&](const f32x4* from, unsigned char* to, unsigned char* scales_to) {
+      const f32x4 lo = from[token * 8 + 2 * (threadIdx.x & 3)], hi = from[token * 8 + 2 * (threadIdx.x & 3) + 1];
+      float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+      const unsigned s = scale_byte(block_magnitude(v, quad_maximum));
+      const float scale = scale_value(s);
+      if (!real) return;
+      *reinterpret_cast<uint2*>(to + (size_t)t * O + f) = make_uint2(to_codes(v[0], v[1], v[2], v[3], scale), to_codes(v[4], v[5], v[6], v[7], scale));
+      if ((threadIdx.x & 3) == 0) scales_to[(size_t)t * scales + f / kScaleBlock] = (unsigned char)s;
+    };
+    if (a.z_scales) keep(staged, static_cast<unsigned char*>(a.z), a.z_scales);
+    if (a.y_codes) keep(staged + kTokens * 8, a.y_codes, a.y_scales);
+  }
 }
 template <int kRows, int kFA, int kFB>
 hipError_t launch_few(LinearArgs a, hipStream_t stream) {
@@ -648,10 +678,13 @@ FewChoice few_as(int T, int O, int K) {
   return {2.6 + (double)((groups + 255) / 256) * bytes / 35e3, launch_few<kRows, kFA, kFB>};
 }
 constexpr int kFewTokens = 1024;   // (a grid's second dimension; more are never faster so)
-FewChoice choose_few(int T, int O, int K) {
+FewChoice choose_few(int T, int O, int K, bool codes) {
   FewChoice best = {1e30, nullptr};
+  for (const FewChoice& c : {few_as<16, 2, 1>(T, O, K), few_as<16, 2, 2>(T, O, K), few_as<16, 2, 4>(T, O, K)})
+    if (c.cost < best.cost) best = c;
+  if (codes) return best;   // (those have whole scale blocks)
   for (const FewChoice& c : {few_as<4, 1, 1>(T, O, K), few_as<8, 1, 1>(T, O, K), few_as<16, 1, 1>(T, O, K), few_as<16, 1, 2>(T, O, K),
-                             few_as<16, 1, 4>(T, O, K), few_as<16, 2, 2>(T, O, K), few_as<16, 2, 4>(T, O, K)})
+                             few_as<16, 1, 4>(T, O, K)})
     if (c.cost < best.cost) best = c;
   return best;
 }
@@ -678,7 +711,7 @@ SplitChoice choose_split(int T, int O, int K) {
   return best;
 }
 
-// How a forward product is computed, by its sizes (and whether results in 8 bits are wanted, which few tokens' kernels do not give).
+// How a forward product is computed, by its sizes (and whether results in 8 bits are wanted).
 struct ForwardPlan {
   ProductChoice tiles;
   FewChoice few;      // if its launch is not null
@@ -687,7 +720,7 @@ struct ForwardPlan {
 ForwardPlan plan_forward(int T, int O, int K, bool codes) {
   ForwardPlan p = {choose_product<false>(T, O, K), {1e30, nullptr}, choose_split(T, O, K)};
   if (p.split.cost >= p.tiles.cost) p.split = {p.tiles.cost, 0, 0};
-  if (T <= kFewTokens && !codes) p.few = choose_few(T, O, K);
+  if (T <= kFewTokens) p.few = choose_few(T, O, K, codes);
   if (p.few.cost < p.split.cost + 3.0) p.split.splits = 0;
   else p.few.launch = nullptr;
   return p;

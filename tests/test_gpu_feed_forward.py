@@ -172,7 +172,7 @@ def test_what_is_not_finite_stays_in_its_row(K):
     print(f"not finite, contraction of {K}", flush=True)
     i = Inputs(K, 2, 80, K, 96, "tail")
     i.flags[1, 5] = PAD
-    want, _ = mate.linear(i.x, i.w, i.bias, i.flags)
+    want, _ = mate.linear(i.x, i.w, i.bias, i.flags, keep_z=mate.MATE_KEEP_8BIT)   # (the same call: the order of the sums goes by sizes and what is kept)
     x, w = i.x.clone(), i.w.clone()
     x[0, 3, -1], x[0, 70, 0], x[1, 5] = math.nan, math.inf, math.nan
     w[7, -1] = math.inf
@@ -675,3 +675,12 @@ def test_split_contractions_again_together_and_in_graphs():
     sick = torch.zeros(B, N, dtype=torch.bool, device="cuda")
     sick[0, 3] = sick[0, 5] = True
     assert torch.equal(torch.isfinite(y).all(-1), ~sick) and torch.equal(torch.isnan(mate.checkpoint_unpack(z)).any(-1), sick)
+
+
+# results in 8 bits of few tokens: a last scale block of 8, 16, 24 features or all 32, one to more than one token tile of each height
+@pytest.mark.parametrize("B,N,E,F", [(1, 1, 8, 8), (1, 1, 768, 776), (3, 4, 1656, 2360), (1, 16, 4096, 48), (1, 17, 72, 88), (5, 13, 264, 1288),
+                                     (3, 101, 3344, 216), (7, 100, 360, 272), (2, 512, 520, 136), (1, 9, 65536, 40), (2, 1, 8, 65536)])
+def test_few_tokens_in_8_bits(B, N, E, F):
+    check_forward(E + N, B, N, E, F, "silu", padding="scattered")
+    check_forward(E + N + 1, B, N, E, F, "gelu", padding="tail", bias=False, residual=False, keep_z=1, keep_y=True)
+    check_forward(E + N + 2, B, N, E, F, "tanh", padding="all", keep_z=2, keep_y=False)
