@@ -666,7 +666,8 @@ hipError_t launch_few(LinearArgs a, hipStream_t stream) {
 // us of a launch, beside those of tiles (which need three that their costs leave out): a unit reads its workgroups' rows at 35 GB/s.  Over 96
 // products of 1 to 1024 tokens and eight pairs of widths (in a graph, weights not in the L2) what it takes is 2 % behind the best form in the
 // mean, 24 % at most (where all take 3 to 4 us).  us, whole tiles and so: 1 token 768 -> 768 7.1 and 3.1, 128 8.0 and 4.5, 512 8.4 and 7.0; 1024 -> 4096 at 16
-// 8.2 and 4.7, at 64 8.9 and 6.5; 4096 -> 1024 at 1 21 and 4.7, at 256 22 and 17.
+// 8.2 and 4.7, at 64 8.9 and 6.5; 4096 -> 1024 at 1 21 and 4.7, at 256 22 and 17; with z in 8 bits (and read back, 2.5) 303 tokens 3344 -> 216 18.7 and
+// 12.6, 12 tokens 1656 -> 2360 15.2 and 9.1.
 struct FewChoice {
   double cost;
   hipError_t (*launch)(LinearArgs, hipStream_t);
