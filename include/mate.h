@@ -382,7 +382,7 @@ mate_status mate_out_project_bwd(const void* o, const void* w_o, const uint8_t* 
  *   residual  gradient that reached x on another way, [B, N, E] bf16, or NULL; may be dx itself
  *   dx, dw, dbias   any may be NULL (not computed); dbias needs dw
  *   workspace mate_linear_bwd_workspace_bytes(B, N, E, F, x_scales != NULL) bytes (0: sizes out of range), at any address;
- *             needed for dw only
+ *             without dw mate_linear_bwd_dx_workspace_bytes(B, N, E, F) do (0: none is needed, as for most sizes)
  * As ever, calls that may run at the same time need workspaces of their own; one after the other they may share one, captured ones too.
  * A layer y = act(x w^T + b) whose next product is y w2^T: mate_linear_bwd of the second with z and act of the first gives the
  * gradient at z, which is dy of the first one's mate_linear_bwd.  The result does not depend on whether the other gradient is wanted.
@@ -410,6 +410,7 @@ mate_status mate_linear(const void* x, const void* w, const float* bias, const u
                         mate_dtype t, void* y, void* z, uint8_t* z_scales, uint8_t* y_codes,
                         uint8_t* y_scales, void* workspace, size_t workspace_bytes, void* stream);
 size_t mate_linear_bwd_workspace_bytes(int B, int N, int E, int F, int x_in_codes);
+size_t mate_linear_bwd_dx_workspace_bytes(int B, int N, int E, int F);
 mate_status mate_linear_bwd(const void* dy, const void* x, const uint8_t* x_scales, const void* w,
                             const uint8_t* flags, const void* z, const uint8_t* z_scales,
                             const void* residual, int B, int N, int E, int F, mate_activation act,

@@ -342,6 +342,11 @@ size_t mate_linear_bwd_workspace_bytes(int B, int N, int E, int F, int x_in_code
   return linear_bwd_workspace(B * N, E, F, x_in_codes != 0);
 }
 
+size_t mate_linear_bwd_dx_workspace_bytes(int B, int N, int E, int F) {
+  if (!tokens_ok(B, N) || !width_ok(E) || !width_ok(F)) return 0;
+  return linear_bwd_dx_workspace(B * N, E, F);
+}
+
 mate_status mate_linear_bwd(const void* dy, const void* x, const uint8_t* x_scales, const void* w,
                             const uint8_t* flags, const void* z, const uint8_t* z_scales,
                             const void* residual, int B, int N, int E, int F, mate_activation act,
@@ -352,7 +357,8 @@ mate_status mate_linear_bwd(const void* dy, const void* x, const uint8_t* x_scal
   if (t != MATE_BF16 || !width_ok(E) || !width_ok(F) || !act_ok(act) || (act == MATE_ACT_NONE) != (z == nullptr) ||
       !aligned({dy, x, w, z, residual, dx, dw, dbias}))
     return MATE_ERR_UNSUPPORTED;
-  if (dw && (!workspace || workspace_bytes < linear_bwd_workspace(B * N, E, F, x_scales != nullptr))) return MATE_ERR_WORKSPACE;
+  const size_t need = dw ? linear_bwd_workspace(B * N, E, F, x_scales != nullptr) : dx ? linear_bwd_dx_workspace(B * N, E, F) : 0;
+  if (need && (!workspace || workspace_bytes < need)) return MATE_ERR_WORKSPACE;
   const LinearBwdCall c = {dy, x, x_scales, w, flags, z, z_scales, residual, B * N, E, F, act, dx, dw, dbias, workspace, next_ticket()};
   return done(launch_linear_bwd(c, static_cast<hipStream_t>(stream)));
 }

@@ -34,6 +34,7 @@ namespace {
   X(mate_dense_workspace_bytes) X(mate_attn_fwd_dense) X(mate_attn_bwd_dense) X(mate_qkv_project) \
   X(mate_out_project) X(mate_project_bwd_workspace_bytes) X(mate_qkv_project_bwd)                 \
   X(mate_out_project_bwd) X(mate_linear_workspace_bytes) X(mate_linear) X(mate_linear_bwd_workspace_bytes) \
+  X(mate_linear_bwd_dx_workspace_bytes) \
   X(mate_linear_bwd) X(mate_activation_bwd) X(mate_checkpoint_pack) X(mate_checkpoint_unpack)
 struct Abi {
 #define X(name) decltype(&::name) name;
@@ -615,17 +616,19 @@ PyObject* linear_bwd(Args a) {  // dy, x, w, flags, z, act, residual, want_dx, w
   if (want_dw) dw = new_tensor({F, E}, at::kFloat, dy);
   if (want_db) db = new_tensor({F}, at::kFloat, dy);
   at::Tensor ws;
-  if (want_dw) {
-    const size_t need = abi.mate_linear_bwd_workspace_bytes(s.B, s.N, E, F, x.scales != nullptr);
-    if (a[10] == Py_None) ws = new_tensor({(int64_t)std::max<size_t>(need, 16)}, at::kByte, dy);
-    else {
-      ws = tensor(a[10], "ws");
-      d.of(ws, at::kByte, ws.sizes(), "ws");
-    }
+  void* pws = nullptr;
+  size_t ws_bytes = 0;
+  if (a[10] != Py_None) {
+    ws = tensor(a[10], "ws");
+    pws = d.of(ws, at::kByte, ws.sizes(), "ws");
+    ws_bytes = (size_t)ws.numel();
+  } else if ((ws_bytes = want_dw   ? abi.mate_linear_bwd_workspace_bytes(s.B, s.N, E, F, x.scales != nullptr)
+                         : want_dx ? abi.mate_linear_bwd_dx_workspace_bytes(s.B, s.N, E, F)
+                                   : 0)) {
+    ws = new_tensor({(int64_t)ws_bytes}, at::kByte, dy);
+    pws = ws.data_ptr();
   }
-  void *pdx = want_dx ? dx.data_ptr() : nullptr, *pdw = want_dw ? dw.data_ptr() : nullptr, *pdb = want_db ? db.data_ptr() : nullptr,
-       *pws = want_dw ? ws.data_ptr() : nullptr;
-  const size_t ws_bytes = want_dw ? (size_t)ws.numel() : 0;
+  void *pdx = want_dx ? dx.data_ptr() : nullptr, *pdw = want_dw ? dw.data_ptr() : nullptr, *pdb = want_db ? db.data_ptr() : nullptr;
   void* st = d.stream();
   call("mate_linear_bwd", [&] {
     return abi.mate_linear_bwd(pg, x.p, x.scales, pw, (uint8_t*)pf, z.p, z.scales, pr, s.B, s.N, E, F, (mate_activation)act, MATE_BF16, pdx,

@@ -154,6 +154,7 @@ struct LinearBwdCall {
   unsigned long long ticket;   // see arrival.h
 };
 size_t linear_bwd_workspace(int T, int E, int F, bool codes);
+size_t linear_bwd_dx_workspace(int T, int E, int F);   // for dx alone
 hipError_t launch_linear_bwd(const LinearBwdCall& c, hipStream_t stream);
 hipError_t launch_activation_bwd(const void* dy, const void* z, const unsigned char* z_scales, const unsigned char* flags, int rows, int E, int act,
                                  void* dz, hipStream_t stream);

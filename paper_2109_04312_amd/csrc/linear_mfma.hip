@@ -461,31 +461,41 @@ hipError_t launch_product(LinearArgs a, hipStream_t stream) {
 
 // Few tiles of a long contraction: each is shared by the workgroups of several ranges of it, whose sums the launch adds.  Ranges of all
 // tiles follow each other, so that every XCD has the same tiles in each.
-template <class S>
+template <class S, bool kGrad>
+__device__ __forceinline__ void split_tile(const LinearStart& p, const LinearArgs& a, const RangeMerge& m, char* lds, int range, int token_tile, int feature_tile) {
+  const int stages = (p.K + 63) >> 6;
+  linear_tile<S, kGrad>(p, a, lds, token_tile * S::kRowsB, feature_tile * S::kRowsA, stages * range / m.splits,
+                        min(p.K, 64 * (stages * (range + 1) / m.splits)), [&](f32x4 (&sum)[S::kFA][S::kOutB], int wave_id) {
+                          float none[S::kFB] = {};
+                          return merge_ranges<S>(m, range, token_tile * p.deal.features + feature_tile, 0, false, sum, none, wave_id);
+                        });
+}
+template <class S, bool kGrad>
 __global__ __launch_bounds__(S::kThreads, S::kAllWaves / 4 * S::kPerCU) void linear_split_kernel(const unsigned short* w, const unsigned short* tok, int T,
                                                                                                int O, int K, int token_tiles, int feature_tiles,
                                                                                                int whole_rows, int by_feature, RangeMerge m, LinearArgs a) {
   extern __shared__ __attribute__((aligned(1024))) char lds[];
   const LinearStart p = {w, tok, T, O, K, {token_tiles, feature_tiles, whole_rows, by_feature}};
   int y, token_tile, feature_tile;
-  const int range = uniform_div(blockIdx.y, p.deal.grid_y(), y), stages = (K + 63) >> 6;
-  if (!dealt_tile(p.deal, blockIdx.x, y, token_tile, feature_tile)) return;
-  linear_tile<S, false>(p, a, lds, token_tile * S::kRowsB, feature_tile * S::kRowsA, stages * range / m.splits, min(K, 64 * (stages * (range + 1) / m.splits)),
-                        [&](f32x4 (&sum)[S::kFA][S::kOutB], int wave_id) {
-                          float none[S::kFB] = {};
-                          return merge_ranges<S>(m, range, token_tile * feature_tiles + feature_tile, 0, false, sum, none, wave_id);
-                        });
+  const int range = uniform_div(blockIdx.y, p.deal.grid_y(), y);
+  if (dealt_tile(p.deal, blockIdx.x, y, token_tile, feature_tile)) split_tile<S, kGrad>(p, a, m, lds, range, token_tile, feature_tile);
 }
 template <class S>
+RangeMerge merge_in(void* workspace, size_t tiles, int splits, unsigned long long ticket) {
+  RangeMerge m = {static_cast<float*>(workspace), nullptr, nullptr, ticket, splits, (int)tiles, 0};
+  m.arrived = reinterpret_cast<unsigned long long*>(m.part + (size_t)splits * tiles * S::kRowsA * S::kRowsB);
+  return m;
+}
+template <class S>
+size_t merge_bytes(size_t tiles, int splits) { return tiles * (splits * (size_t)(S::kRowsA * S::kRowsB * 4) + kMaxRanges * 8); }
+template <class S, bool kGrad>
 hipError_t launch_split(LinearArgs a, int splits, void* workspace, unsigned long long ticket, hipStream_t stream) {
   deal_tiles<S>(a);
   const TileDeal& d = a.deal;
-  const int tiles = d.tokens * d.features;
-  RangeMerge m = {static_cast<float*>(workspace), nullptr, nullptr, ticket, splits, tiles, 0};
-  m.arrived = reinterpret_cast<unsigned long long*>(m.part + (size_t)splits * tiles * S::kRowsA * S::kRowsB);
-  const hipError_t e = allow_lds<&linear_split_kernel<S>>(S::kLds);
+  const RangeMerge m = merge_in<S>(workspace, (size_t)d.tokens * d.features, splits, ticket);
+  const hipError_t e = allow_lds<&linear_split_kernel<S, kGrad>>(S::kLds);
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((linear_split_kernel<S>), dim3(d.grid_x(), d.grid_y() * splits), dim3(S::kThreads), S::kLds, stream, a.w, a.tok, a.T, a.O, a.K,
+  hipLaunchKernelGGL((linear_split_kernel<S, kGrad>), dim3(d.grid_x(), d.grid_y() * splits), dim3(S::kThreads), S::kLds, stream, a.w, a.tok, a.T, a.O, a.K,
                      d.tokens, d.features, d.rows, d.by_feature, m, a);
   return hipGetLastError();
 }
@@ -707,7 +717,7 @@ SplitChoice choose_split(int T, int O, int K) {
   for (int splits = 2; splits <= kMaxRanges && tiles * splits <= 256 && stages >= 16 * splits; ++splits) {
     double cost = (stages + splits - 1) / splits * 0.29 + 0.9;
     for (int r = 1; r < splits; r *= 2) cost += 2.6 + 0.6 * (double)(tiles * splits) / 256;   // one addition of pairs
-    if (cost < best.cost) best = {cost, splits, tiles * (splits * (size_t)(TileSplit::kRowsA * TileSplit::kRowsB * 4) + kMaxRanges * 8)};
+    if (cost < best.cost) best = {cost, splits, merge_bytes<TileSplit>(tiles, splits)};
   }
   return best;
 }
@@ -987,15 +997,19 @@ using Wgrad256 = Shape<4, 4, 2, 4, 2, 1>;      // 256 x 256
 using Wgrad128 = Shape<2, 2, 2, 2, 2, 1, 2>;   // 128 x 128, two groups
 
 template <class S, bool kCodes>
-__global__ __launch_bounds__(S::kThreads, S::kAllWaves / 4) void linear_bwd_kernel(WeightGradArgs w, LinearArgs a, int w_groups) {
+__global__ __launch_bounds__(S::kThreads, S::kAllWaves / 4) void linear_bwd_kernel(WeightGradArgs w, LinearArgs a, RangeMerge m, int w_groups) {
   extern __shared__ __attribute__((aligned(1024))) char lds[];
   static_assert(S::kThreads == Wgrad128::kThreads, "one workgroup size for both");
   if ((int)blockIdx.x < w_groups) {
     weight_grad_tile<Wgrad128, true, kCodes>(w, lds, blockIdx.x);
   } else {
-    int x, token_tile, feature_tile;
-    const int y = uniform_div(blockIdx.x - w_groups, a.deal.grid_x(), x);
-    if (dealt_tile(a.deal, x, y, token_tile, feature_tile)) linear_tile<S, true>(a, a, lds, token_tile * S::kRowsB, feature_tile * S::kRowsA);
+    int x, token_tile, feature_tile, at = blockIdx.x - w_groups;
+    const int range = S::kB == 1 && m.splits > 1 ? uniform_div(at, a.deal.grid_x() * a.deal.grid_y(), at) : 0;
+    const int y = uniform_div(at, a.deal.grid_x(), x);
+    if (!dealt_tile(a.deal, x, y, token_tile, feature_tile)) return;
+    if constexpr (S::kB == 1)
+      if (m.splits > 1) return split_tile<S, true>(a, a, m, lds, range, token_tile, feature_tile);
+    linear_tile<S, true>(a, a, lds, token_tile * S::kRowsB, feature_tile * S::kRowsA);
   }
 }
 
@@ -1007,8 +1021,10 @@ struct BackwardPlan {
   bool one_launch;
   int splits, per_split, tile;   // of dw
   ProductChoice product;         // of dx
+  int dx_splits;                 // ranges of its contraction, each of 16 stages or more (1, or in one launch, by tiles of 64 tokens)
   bool copy;                     // x in 8 bits is brought back first
-  size_t bias_off, words_off, copy_off, total;
+  size_t bias_off, words_off, copy_off, dx_off, total;
+  size_t dx_bytes;               // what dx needs alone
 };
 // When the last of `first` workgroups of t1 us and then `second` ones of t2 us ends, one at a time on each unit.
 double end_of_both(int first, double t1, long second, double t2) {
@@ -1029,10 +1045,11 @@ BackwardPlan plan_backward(int T, int E, int F, bool codes) {
   const long blocks = (T + 63L) / 64;
   constexpr int kSlots = 256;
   p.product = choose_product<true>(T, E, F);
+  p.dx_splits = 1;
   // Two launches: large tiles read half as much per contraction, small ones need fewer ranges, and every range leaves an fp32
   // matrix that is written and read again.  In us, one workgroup a compute unit: 1.45 a token block for 256 x 256, 0.58 for
   // 128 x 128 with two groups, 1 per 6.5 MB of partial sums.  (Measured and so, both gradients: 4072 tokens 2048 -> 768 43.6 and 45, 768 -> 2048 41
-  // and 47, 2048 tokens 768 -> 768 22.0 and 21.5, 512 17.1 and 17.5, 512 tokens 1024 -> 4096 37 and 38.)
+  // and 47, 2048 tokens 768 -> 768 22.0 and 21.5, 512 17.1 and 17.5.)
   double two = 1e30;
   for (int tile : {256, 128}) {
     const long tiles = tiles_of_size(F, E, tile);
@@ -1058,17 +1075,28 @@ BackwardPlan plan_backward(int T, int E, int F, bool codes) {
       const int first = (int)((tiles * ranges + 7) / 8 * 8);
       double t1 = (0.44 + 0.12 * std::min(1.0, first / 256.0)) * ((blocks + ranges - 1) / ranges) + 5.1;
       for (int r = 1; r < ranges; r *= 2) t1 += 2.7;   // one addition of pairs
-      for (const ProductChoice& c : {product_as<Tile128x2, true>(T, E, F, 0.38, 0, 3.1), product_as<Tile64x2, true>(T, E, F, 0.35, 0, 1.8)}) {
+      auto consider = [&](const ProductChoice& c, int dx_splits, double dx_cost) {
         // (padding, which this leaves out, shortens long ranges most: several must be worth 16 %)
-        const double cost = (ranges > 1 ? 1.16 : 1.0) * (0.5 + end_of_both(first, t1, c.tiles, c.tile_cost));
-        if (cost < two) {
-          two = cost;
-          p.one_launch = true;
-          p.splits = ranges;
-          p.tile = 128;
-          p.per_split = (int)blocks;
-          p.product = c;
-        }
+        const double cost = (ranges > 1 ? 1.16 : 1.0) * (0.5 + end_of_both(first, t1, c.tiles * dx_splits, dx_cost));
+        if (cost >= two) return;
+        two = cost;
+        p.one_launch = true;
+        p.splits = ranges;
+        p.tile = 128;
+        p.per_split = (int)blocks;
+        p.product = c;
+        p.dx_splits = dx_splits;
+      };
+      const ProductChoice tall = product_as<Tile128x2, true>(T, E, F, 0.38, 0, 3.1), low = product_as<TileSplit, true>(T, E, F, 0.35, 0, 1.8);
+      consider(tall, 1, tall.tile_cost);
+      consider(low, 1, low.tile_cost);
+      // (dx of a long contraction in ranges too.  us, both gradients with a whole contraction and so: 32 tokens 216 -> 3656 24.3 and 15.4, 300 tokens
+      // 520 -> 4104 30.7 and 20.9, 512 tokens 1024 -> 4096 33.3 and 26.2, 768 -> 2048 15.5 and 13.5; dx alone 24.6 and 15.0, 30.0 and 17.5, 25.7 and 16.3, 14.7 and 12.4)
+      const int dx_stages = (F + 63) / 64;
+      for (int n = 2; n <= kMaxRanges && dx_stages >= 16 * n && low.tiles * n <= kSlots; ++n) {
+        double cost = (dx_stages + n - 1) / n * 0.35 + 1.8;
+        for (int r = 1; r < n; r *= 2) cost += 2.7;
+        consider(low, n, cost);
       }
     }
   const long rows = (F + p.tile - 1) / p.tile * p.tile, columns = (E + p.tile - 1) / p.tile * p.tile;   // whole tiles
@@ -1080,7 +1108,10 @@ BackwardPlan plan_backward(int T, int E, int F, bool codes) {
   p.copy_off = align256(p.total);
   const double rounds = (double)((tiles_of_size(F, E, p.tile) * p.splits + kSlots - 1) / kSlots), stages = (double)((blocks + p.splits - 1) / p.splits);
   p.copy = 0.36 * rounds * stages > 2.5 + 3.0 * T * E / 4.6e6;
-  p.total = p.copy_off + (p.copy && codes ? (size_t)T * E * 2 : 0) + 256;
+  p.dx_off = align256(p.copy_off + (p.copy && codes ? (size_t)T * E * 2 : 0));
+  const size_t dx_part = p.dx_splits > 1 ? merge_bytes<TileSplit>((size_t)p.product.tiles, p.dx_splits) : 0;
+  p.dx_bytes = dx_part ? dx_part + 16 : 0;
+  p.total = p.dx_off + dx_part + 256;
   return p;
 }
 
@@ -1094,21 +1125,25 @@ hipError_t launch_weight_grad(const WeightGradArgs& a, hipStream_t stream) {
   return hipGetLastError();
 }
 template <class S, bool kCodes>
-hipError_t launch_both(const WeightGradArgs& w, LinearArgs a, hipStream_t stream) {
+hipError_t launch_both(const WeightGradArgs& w, LinearArgs a, int dx_splits, void* dx_workspace, hipStream_t stream) {
   deal_tiles<S>(a);
   const int w_groups = (int)((tiles_of_size(w.F, w.E, 128) * w.splits + 7) / 8 * 8);   // (whole rounds of XCDs, so that the products' tiles are dealt as ever)
   constexpr int kLds = std::max(S::kLds, Wgrad128::kLds);
   const hipError_t e = allow_lds<&linear_bwd_kernel<S, kCodes>>(kLds);
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((linear_bwd_kernel<S, kCodes>), dim3(w_groups + a.deal.grid_x() * a.deal.grid_y()), dim3(S::kThreads), kLds, stream, w, a, w_groups);
+  const RangeMerge m = merge_in<S>(dx_workspace, (size_t)a.deal.tokens * a.deal.features, dx_splits, w.ticket);
+  hipLaunchKernelGGL((linear_bwd_kernel<S, kCodes>), dim3(w_groups + a.deal.grid_x() * a.deal.grid_y() * dx_splits), dim3(S::kThreads), kLds, stream, w, a, m,
+                     w_groups);
   return hipGetLastError();
 }
 template <bool kCodes>
-hipError_t run_backward(const BackwardPlan& p, const WeightGradArgs& w, LinearArgs a, hipStream_t stream) {
+hipError_t run_backward(const BackwardPlan& p, const WeightGradArgs& w, LinearArgs a, void* dx_workspace, hipStream_t stream) {
   if (p.one_launch && w.out) {
     if (!a.y) return launch_weight_grad<Wgrad128, true, kCodes>(w, stream);
-    return p.product.rows == 128 ? launch_both<Tile128x2, kCodes>(w, a, stream) : launch_both<Tile64x2, kCodes>(w, a, stream);
+    return p.product.rows == 128 ? launch_both<Tile128x2, kCodes>(w, a, 1, nullptr, stream)
+                                 : launch_both<TileSplit, kCodes>(w, a, p.dx_splits, dx_workspace, stream);
   }
+  if (a.y && p.dx_splits > 1) return launch_split<TileSplit, true>(a, p.dx_splits, dx_workspace, w.ticket, stream);   // (without dw)
   if (w.out) {
     const hipError_t e = p.tile == 256 ? launch_weight_grad<Wgrad256, false, kCodes>(w, stream) : launch_weight_grad<Wgrad128, false, kCodes>(w, stream);
     if (e != hipSuccess) return e;
@@ -1141,7 +1176,7 @@ hipError_t launch_linear(const LinearCall& c, hipStream_t stream) {
   if (p.few.launch) return p.few.launch(a, stream);
   if (!p.split.splits) return p.tiles.launch(a, stream);
   char* ws = static_cast<char*>(c.workspace);
-  return launch_split<TileSplit>(a, p.split.splits, ws + (-reinterpret_cast<uintptr_t>(ws) & 15), c.ticket, stream);
+  return launch_split<TileSplit, false>(a, p.split.splits, ws + (-reinterpret_cast<uintptr_t>(ws) & 15), c.ticket, stream);
 }
 size_t linear_workspace(int T, int E, int F, bool codes) {
   const ForwardPlan p = plan_forward(T, F, E, codes);
@@ -1149,6 +1184,7 @@ size_t linear_workspace(int T, int E, int F, bool codes) {
 }
 
 size_t linear_bwd_workspace(int T, int E, int F, bool codes) { return plan_backward(T, E, F, codes).total; }   // (the caller's address may be any)
+size_t linear_bwd_dx_workspace(int T, int E, int F) { return plan_backward(T, E, F, false).dx_bytes; }
 
 hipError_t launch_linear_bwd(const LinearBwdCall& c, hipStream_t stream) {
   const BackwardPlan p = plan_backward(c.T, c.E, c.F, c.x_scales != nullptr);
@@ -1184,7 +1220,8 @@ hipError_t launch_linear_bwd(const LinearBwdCall& c, hipStream_t stream) {
     w.x = ws + p.copy_off;
     w.x_scales = nullptr;
   }
-  return w.x_scales ? run_backward<true>(p, w, a, stream) : run_backward<false>(p, w, a, stream);
+  void* const dx_workspace = c.dw ? ws + p.dx_off : ws;
+  return w.x_scales ? run_backward<true>(p, w, a, dx_workspace, stream) : run_backward<false>(p, w, a, dx_workspace, stream);
 }
 
 }  // namespace mate

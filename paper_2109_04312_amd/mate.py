@@ -29,7 +29,7 @@ MATE_MAX_N, MATE_MAX_HEADS, MATE_HEAD_DIM = 16384, 256, 64
 EXPORTS = ["mate_segments_bytes", "mate_workspace_bytes", "mate_build_segments",
            "mate_build_segments_bucketed", "mate_cell_positions", "mate_segments_export", "mate_segments_export_windows", "mate_attn_fwd", "mate_attn_bwd", "mate_dense_workspace_bytes",
            "mate_attn_fwd_dense", "mate_attn_bwd_dense", "mate_attn_bwd_dense_static", "mate_attn_prefers_dense", "mate_segments_status", "mate_qkv_project", "mate_out_project", "mate_project_bwd_workspace_bytes", "mate_qkv_project_bwd", "mate_out_project_bwd",
-           "mate_linear_workspace_bytes", "mate_linear", "mate_linear_bwd_workspace_bytes", "mate_linear_bwd", "mate_activation_bwd", "mate_checkpoint_pack", "mate_checkpoint_unpack", "mate_profile_kernel",
+           "mate_linear_workspace_bytes", "mate_linear", "mate_linear_bwd_workspace_bytes", "mate_linear_bwd_dx_workspace_bytes", "mate_linear_bwd", "mate_activation_bwd", "mate_checkpoint_pack", "mate_checkpoint_unpack", "mate_profile_kernel",
            "mate_probe_mfma", "mate_status_string"]
 MATE_KERNEL_NONE, MATE_KERNEL_BUILD, MATE_KERNEL_FWD = 0, 1, 2
 MATE_KERNEL_BWD_DQ, MATE_KERNEL_BWD_DKV = 3, 4
@@ -102,6 +102,8 @@ _lib.mate_linear.restype = _i
 _lib.mate_linear.argtypes = [_p, _p, _p, _p, _p, _i, _i, _i, _i, _i, _i, _p, _p, _p, _p, _p, _p, _sz, _p]
 _lib.mate_linear_bwd_workspace_bytes.restype = _sz
 _lib.mate_linear_bwd_workspace_bytes.argtypes = [_i, _i, _i, _i, _i]
+_lib.mate_linear_bwd_dx_workspace_bytes.restype = _sz
+_lib.mate_linear_bwd_dx_workspace_bytes.argtypes = [_i, _i, _i, _i]
 _lib.mate_linear_bwd.restype = _i
 _lib.mate_linear_bwd.argtypes = [_p, _p, _p, _p, _p, _p, _p, _p, _i, _i, _i, _i, _i, _i, _p, _p, _p, _p, _sz, _p]
 _lib.mate_activation_bwd.restype = _i
@@ -143,6 +145,7 @@ mate_out_project_bwd = _lib.mate_out_project_bwd
 mate_linear_workspace_bytes = _lib.mate_linear_workspace_bytes
 mate_linear = _lib.mate_linear
 mate_linear_bwd_workspace_bytes = _lib.mate_linear_bwd_workspace_bytes
+mate_linear_bwd_dx_workspace_bytes = _lib.mate_linear_bwd_dx_workspace_bytes
 mate_linear_bwd = _lib.mate_linear_bwd
 mate_activation_bwd = _lib.mate_activation_bwd
 mate_checkpoint_pack = _lib.mate_checkpoint_pack
@@ -300,7 +303,7 @@ def linear_bwd(dy, x, w, flags=None, z=None, act=MATE_ACT_NONE, residual=None, w
     """Gradients of linear() at its pre-activation, dy [B,N,F] bf16: dx = (dy w) act'(z) + residual [B,N,E] bf16, dw = sum dy^T x
     [F,E] float32, dbias [F] float32 (None for the ones not wanted).  x (bf16 or a Checkpoint; None if dw is not wanted) is what
     the product read; if that was an activation, x = act(z), z (bf16 or a Checkpoint) makes dx the gradient at z.  residual: a
-    gradient that reached x on another way."""
+    gradient that reached x on another way.  ws: linear_bwd_workspace()."""
     return _native.linear_bwd(dy, x, w, flags, z, act, residual, want_dx, want_dw, want_dbias, ws)
 
 

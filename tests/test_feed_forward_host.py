@@ -49,6 +49,12 @@ def test_linear_bwd():
     need = mate.mate_linear_bwd_workspace_bytes(2, 100, 768, 1000, 1)
     assert need > 0
     refuses(mate.mate_linear_bwd, ok, [(18, need - 1, mate.MATE_ERR_WORKSPACE)])
+    alone = list(ok)                                             # dx alone, at sizes where it needs a workspace
+    alone[8:12], alone[15], alone[16] = [1, 32, 216, 4096], None, None
+    need = mate.mate_linear_bwd_dx_workspace_bytes(1, 32, 216, 4096)
+    assert 0 < need < mate.mate_linear_bwd_workspace_bytes(1, 32, 216, 4096, 1)
+    refuses(mate.mate_linear_bwd, alone, [(17, None, mate.MATE_ERR_WORKSPACE), (18, need - 1, mate.MATE_ERR_WORKSPACE)])
+    assert mate.mate_linear_bwd_dx_workspace_bytes(2, 100, 768, 1000) == mate.mate_linear_bwd_dx_workspace_bytes(1, 32, 212, 4096) == 0
     assert mate.mate_linear_bwd_workspace_bytes(2, 100, 765, 1000, 0) == 0
     assert mate.mate_linear_bwd_workspace_bytes(0, 100, 768, 1000, 0) == 0
     with pytest.raises(mate.MateError):

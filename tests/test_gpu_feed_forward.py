@@ -684,3 +684,39 @@ def test_few_tokens_in_8_bits(B, N, E, F):
     check_forward(E + N, B, N, E, F, "silu", padding="scattered")
     check_forward(E + N + 1, B, N, E, F, "gelu", padding="tail", bias=False, residual=False, keep_z=1, keep_y=True)
     check_forward(E + N + 2, B, N, E, F, "tanh", padding="all", keep_z=2, keep_y=False)
+
+
+# dx of few tokens and a long contraction, shared by two and more ranges beside dw's tiles or alone; a rest for the last range, padding
+@pytest.mark.parametrize("x8", [False, True])
+@pytest.mark.parametrize("B,N,E,F", [(2, 16, 216, 3656), (1, 1, 8, 4096), (9, 26, 264, 2376), (4, 34, 320, 2720), (3, 100, 520, 4104)])
+def test_split_dx(B, N, E, F, x8):
+    mate = mate_module()
+    assert mate.mate_linear_bwd_dx_workspace_bytes(B, N, E, F) > 0
+    check_backward(N, B, N, E, F, "gelu", padding="scattered", residual=N != 16, x8=x8, z8=not x8)
+    check_backward(N + 1, B, N, E, F, "none", padding="all" if x8 else None, x8=x8)
+    i = Inputs(N, B, N, E, F, "scattered")
+    x = mate.checkpoint_pack(i.x) if x8 else i.x
+    kw = dict(z=i.z, act=mate.MATE_ACT_GELU, residual=i.res_x)
+    both = mate.linear_bwd(i.dy, x, i.w, i.flags, **kw)
+    size = mate.mate_linear_bwd_dx_workspace_bytes(B, N, E, F)
+    room = torch.full((size + 7,), 255, dtype=torch.uint8, device="cuda")
+    for ws in (None, room[7:]):
+        alone = mate.linear_bwd(i.dy, None, i.w, i.flags, want_dw=False, want_dbias=False, ws=ws, **kw)
+        assert torch.equal(alone[0], both[0]) and alone[1] is None
+    assert all(torch.equal(u, v) for u, v in zip(mate.linear_bwd(i.dy, x, i.w, i.flags, want_dx=False, **kw)[1:], both[1:]))
+    with pytest.raises(mate.MateError) as e:
+        mate.linear_bwd(i.dy, None, i.w, i.flags, want_dw=False, want_dbias=False, ws=room[:size - 1], **kw)
+    assert e.value.status == mate.MATE_ERR_WORKSPACE
+    ws = torch.full((mate.mate_linear_bwd_workspace_bytes(B, N, E, F, int(x8)) + 9,), 255, dtype=torch.uint8, device="cuda")[9:]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=torch.cuda.Stream()):
+        captured = mate.linear_bwd(i.dy, x, i.w, i.flags, ws=ws, **kw)
+    for replay in range(3):
+        for t in captured:
+            t.fill_(77)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(u, v) for u, v in zip(captured, both)), replay
+        again = mate.linear_bwd(i.dy, x, i.w, i.flags, ws=ws, **kw)
+        torch.cuda.synchronize()
+        assert all(torch.equal(u, v) for u, v in zip(again, both)), replay
