@@ -472,7 +472,8 @@ struct Codes {
   uint8_t *code = nullptr, *scale = nullptr;
   explicit operator bool() const { return code; }
   Codes() = default;
-  Codes(PyObject* o, const OnDevice& d, const Tokens& x, int width, const char* name) {
+  // (Each attribute is asked for once, and kept: one that is computed has no other owner.)
+  explicit Codes(PyObject* o) {
     PyObject *c = PyObject_GetAttr(o, s_codes), *s = c ? PyObject_GetAttr(o, s_scales) : nullptr;
     if (!s) {
       Py_XDECREF(c);
@@ -486,8 +487,8 @@ struct Codes {
     Py_DECREF(c);
     Py_DECREF(s);
     if (!tensors) fail(PyExc_TypeError, "a checkpoint holds two tensors");
-    place(d, x, width, name);
   }
+  Codes(PyObject* o, const OnDevice& d, const Tokens& x, int width, const char* name) : Codes(o) { place(d, x, width, name); }
   static Codes fresh(const OnDevice& d, const Tokens& x, int width, const at::Tensor& like) {
     Codes k;
     k.codes = at::empty(x.with(width), at::TensorOptions(like.device()).dtype(at::kByte));
@@ -667,15 +668,12 @@ PyObject* checkpoint_pack(Args a) {  // x, flags, out
 }
 
 PyObject* checkpoint_unpack(Args a) {  // checkpoint, f32, out
-  PyObject* c = PyObject_GetAttr(a[0], s_codes);
-  if (!c) throw PyFailure();
-  Py_DECREF(c);  // (the checkpoint holds it)
-  const at::Tensor& codes = tensor(c, "codes");
-  const Tokens s(codes, "codes");
+  Codes k(a[0]);
+  const Tokens s(k.codes, "codes");
   const at::ScalarType type = truth(a[1]) ? at::kFloat : at::kBFloat16;
-  const OnDevice d(codes);
-  const Codes k(a[0], d, s, s.W, "checkpoint");
-  at::Tensor x = a[2] == Py_None ? new_tensor({s.B, s.N, s.W}, type, codes) : tensor(a[2], "out");
+  const OnDevice d(k.codes);
+  k.place(d, s, s.W, "checkpoint");
+  at::Tensor x = a[2] == Py_None ? new_tensor({s.B, s.N, s.W}, type, k.codes) : tensor(a[2], "out");
   void *px = d.of(x, type, s.with(s.W), "out"), *st = d.stream();
   call("mate_checkpoint_unpack",
        [&] { return abi.mate_checkpoint_unpack(k.code, k.scale, s.B, s.N, s.W, type == at::kFloat ? MATE_F32 : MATE_BF16, px, st); });
