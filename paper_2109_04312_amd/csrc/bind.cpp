@@ -199,17 +199,24 @@ Ids ids(PyObject* row, PyObject* col, PyObject* flags) {
   return {dev(r, "row_ids"), dev(c, "col_ids"), dev(f, "flags"), (int)f.size(0), (int)f.size(1)};
 }
 
+// An attribute of an object, held: one that is computed has no other owner.
+struct Attribute {
+  PyObject* value;
+  Attribute(PyObject* o, PyObject* name) : value(PyObject_GetAttr(o, name)) {
+    if (!value) throw PyFailure();
+  }
+  ~Attribute() { Py_DECREF(value); }
+  Attribute(const Attribute&) = delete;
+  Attribute& operator=(const Attribute&) = delete;
+};
+
 // The table buffer of a mate.Segments, checked against the tensors' (B, N).
-void* tables(PyObject* seg, int B, int N) {
-  PyObject *buf = PyObject_GetAttr(seg, s_buf), *b = PyObject_GetAttr(seg, s_B), *n = PyObject_GetAttr(seg, s_N);
-  Py_XDECREF(buf);  // the Segments object keeps them alive
-  Py_XDECREF(b);
-  Py_XDECREF(n);
-  if (!buf || !b || !n) throw PyFailure();
-  const at::Tensor& t = tensor(buf, "segments");
-  if (integer(b) != B || integer(n) != N || (size_t)t.numel() < abi.mate_segments_bytes(B, N))
+at::Tensor tables(PyObject* seg, int B, int N) {
+  const Attribute buf(seg, s_buf), b(seg, s_B), n(seg, s_N);
+  const at::Tensor& t = tensor(buf.value, "segments");
+  if (integer(b.value) != B || integer(n.value) != N || (size_t)t.numel() < abi.mate_segments_bytes(B, N))
     check(MATE_ERR_SHAPE, "segment tables are for another (B, N) than the tensors");
-  return t.data_ptr();
+  return t;
 }
 
 // ---- entry points ----------------------------------------------------------------------------
@@ -255,7 +262,7 @@ PyObject* cell_positions(Args a) {  // row, col, flags, out | None
 PyObject* attn_fwd(Args a) {  // q, k, v, seg, head_kind, scale, out, lse, ws
   const at::Tensor& q = tensor(a[0], "q");
   const Shape4 x = shape4(q);
-  void* seg = tables(a[3], x.B, x.N);
+  const at::Tensor seg = tables(a[3], x.B, x.N);
   const HeadKinds hk(a[4], x.H);
   const mate_dtype t = dtype_code(q);
   const float scale = real(a[5]);
@@ -265,7 +272,7 @@ PyObject* attn_fwd(Args a) {  // q, k, v, seg, head_kind, scale, out, lse, ws
   void *pq = dev(q, "q"), *pk = dev(a[1], "k"), *pv = dev(a[2], "v"), *po = dev(out, "out"), *pl = dev(lse, "lse");
   void* s = stream();
   call("mate_attn_fwd", [&] {
-    return abi.mate_attn_fwd(pq, pk, pv, seg, hk.get(), x.B, x.H, x.N, x.D, t, scale, po, (float*)pl, ws.ptr,
+    return abi.mate_attn_fwd(pq, pk, pv, seg.data_ptr(), hk.get(), x.B, x.H, x.N, x.D, t, scale, po, (float*)pl, ws.ptr,
                              ws.bytes, s);
   });
   return pack({out, lse});
@@ -274,7 +281,7 @@ PyObject* attn_fwd(Args a) {  // q, k, v, seg, head_kind, scale, out, lse, ws
 PyObject* attn_bwd(Args a) {  // q, k, v, out, lse, dout, seg, head_kind, scale, dq, dk, dv, ws
   const at::Tensor& q = tensor(a[0], "q");
   const Shape4 x = shape4(q);
-  void* seg = tables(a[6], x.B, x.N);
+  const at::Tensor seg = tables(a[6], x.B, x.N);
   const HeadKinds hk(a[7], x.H);
   const mate_dtype t = dtype_code(q);
   const float scale = real(a[8]);
@@ -284,7 +291,7 @@ PyObject* attn_bwd(Args a) {  // q, k, v, out, lse, dout, seg, head_kind, scale,
        *pg = dev(a[5], "dout"), *pdq = dev(dq, "dq"), *pdk = dev(dk, "dk"), *pdv = dev(dv, "dv");
   void* s = stream();
   call("mate_attn_bwd", [&] {
-    return abi.mate_attn_bwd(pq, pk, pv, po, (const float*)pl, pg, seg, hk.get(), x.B, x.H, x.N, x.D, t, scale, pdq,
+    return abi.mate_attn_bwd(pq, pk, pv, po, (const float*)pl, pg, seg.data_ptr(), hk.get(), x.B, x.H, x.N, x.D, t, scale, pdq,
                              pdk, pdv, ws.ptr, ws.bytes, s);
   });
   return pack({dq, dk, dv});
@@ -472,21 +479,11 @@ struct Codes {
   uint8_t *code = nullptr, *scale = nullptr;
   explicit operator bool() const { return code; }
   Codes() = default;
-  // (Each attribute is asked for once, and kept: one that is computed has no other owner.)
   explicit Codes(PyObject* o) {
-    PyObject *c = PyObject_GetAttr(o, s_codes), *s = c ? PyObject_GetAttr(o, s_scales) : nullptr;
-    if (!s) {
-      Py_XDECREF(c);
-      throw PyFailure();
-    }
-    const bool tensors = THPVariable_Check(c) && THPVariable_Check(s);
-    if (tensors) {
-      codes = THPVariable_Unpack(c);
-      scales = THPVariable_Unpack(s);
-    }
-    Py_DECREF(c);
-    Py_DECREF(s);
-    if (!tensors) fail(PyExc_TypeError, "a checkpoint holds two tensors");
+    const Attribute c(o, s_codes), s(o, s_scales);
+    if (!THPVariable_Check(c.value) || !THPVariable_Check(s.value)) fail(PyExc_TypeError, "a checkpoint holds two tensors");
+    codes = THPVariable_Unpack(c.value);
+    scales = THPVariable_Unpack(s.value);
   }
   Codes(PyObject* o, const OnDevice& d, const Tokens& x, int width, const char* name) : Codes(o) { place(d, x, width, name); }
   static Codes fresh(const OnDevice& d, const Tokens& x, int width, const at::Tensor& like) {

@@ -8,7 +8,7 @@ from paper_2109_04312_amd import mate
 
 
 class Computed:
-    """codes and scales made anew at each access, from memory that others have just used."""
+    """codes, scales and buf made anew at each access, from memory that others have just used."""
     B, N, W = 2, 5, 40
 
     def __init__(self, dims=3):
@@ -25,6 +25,10 @@ class Computed:
     @property
     def scales(self):
         return self.fresh(self.B, self.N, 2)
+
+    @property
+    def buf(self):
+        return self.fresh(mate.mate_segments_bytes(self.B, self.N))
 
 
 class ComputedCheckpoint(Computed, mate.Checkpoint):
@@ -50,3 +54,18 @@ def test_checkpoint_of_no_tensors():
         mate.checkpoint_unpack(mate.Checkpoint(torch.zeros(2, 5, 40, dtype=torch.uint8), 3))
     with pytest.raises(AttributeError):
         mate.checkpoint_unpack(torch.zeros(2, 5, 40))
+
+
+def test_segment_tables():
+    x = torch.zeros(Computed.B, 4, Computed.N, 64, dtype=torch.bfloat16)
+    lse = torch.zeros(Computed.B, 4, Computed.N)
+    for _ in range(20):
+        gc.collect()
+        with pytest.raises(ValueError, match="q must be a contiguous device tensor"):   # the tables themselves are right
+            mate.attn_fwd(x, x, x, Computed(), [0, 0, 1, 1], 0.125, out=x, lse=lse, ws=torch.zeros(16, dtype=torch.uint8))
+        with pytest.raises(ValueError, match="q must be a contiguous device tensor"):
+            mate.attn_bwd(x, x, x, x, lse, x, Computed(), [0, 0, 1, 1], 0.125, dq=x, dk=x, dv=x, ws=torch.zeros(16, dtype=torch.uint8))
+    other = Computed()
+    other.N = Computed.N + 1
+    with pytest.raises(mate.MateError):
+        mate.attn_fwd(x, x, x, other, [0, 0, 1, 1], 0.125)
