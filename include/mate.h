@@ -379,7 +379,8 @@ mate_status mate_out_project_bwd(const void* o, const void* w_o, const uint8_t* 
  *   w         may be NULL if dx is
  *   z         the pre-activation that x came from, x = act(z): [B, N, E] bf16, or codes if z_scales is not NULL; NULL if x is
  *             no activation (act is MATE_ACT_NONE then, and z NULL)
- *   residual  gradient that reached x on another way, [B, N, E] bf16, or NULL; may be dx itself
+ *   residual  gradient that reached z on another way (x itself, if z is NULL), [B, N, E] bf16, or NULL; may be dx itself.  It is added as
+ *             it is: one that reached x = act(z) has to be multiplied with act'(z) before (mate_activation_bwd does, in place)
  *   dx, dw, dbias   any may be NULL (not computed); dbias needs dw
  *   workspace mate_linear_bwd_workspace_bytes(B, N, E, F, x_scales != NULL) bytes (0: sizes out of range), at any address;
  *             without dw mate_linear_bwd_dx_workspace_bytes(B, N, E, F) do (0: none is needed, as for most sizes)

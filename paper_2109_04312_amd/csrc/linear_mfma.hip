@@ -1,6 +1,6 @@
 // The products of a layer's feed-forward half and their gradients, bf16 MFMA (gfx950):
 //   forward:  z = x w^T + bias,  y = act(z) + residual, and what the backward needs of them (z in bf16 or in 8 bits, y in 8 bits);
-//   dx:       (dy w) act'(z) + the residual's gradient, z the pre-activation that x came from;
+//   dx:       (dy w) act'(z) + a gradient that reached z on another way, z the pre-activation that x came from (without one: that reached x);
 //   dw:       sum over tokens of dy^T x, x in bf16 or in 8 bits.
 // The main loop is that of the projections (product.h): C[b, a] = sum_k B[b, k] A[a, k], a contiguous in the output, so that a lane holds
 // four consecutive features of a token.  Rows are flat tokens here, and widths any multiple of 8: a last
@@ -34,7 +34,7 @@ struct LinearStart {
 };
 struct LinearArgs : LinearStart {
   const unsigned char* flags;   // [T] or null
-  const unsigned short* add;    // [T][O] or null: residual, or the residual's gradient
+  const unsigned short* add;    // [T][O] or null: residual, or the gradient that is added to dx
   int act;
   const float* bias;            // forward: [O] or null
   const void* z_in;             // dx: pre-activation [T][O], bf16, or codes if z_in_scales is not null

@@ -303,7 +303,8 @@ def linear_bwd(dy, x, w, flags=None, z=None, act=MATE_ACT_NONE, residual=None, w
     """Gradients of linear() at its pre-activation, dy [B,N,F] bf16: dx = (dy w) act'(z) + residual [B,N,E] bf16, dw = sum dy^T x
     [F,E] float32, dbias [F] float32 (None for the ones not wanted).  x (bf16 or a Checkpoint; None if dw is not wanted) is what
     the product read; if that was an activation, x = act(z), z (bf16 or a Checkpoint) makes dx the gradient at z.  residual: a
-    gradient that reached x on another way.  ws: linear_bwd_workspace()."""
+    gradient that reached z on another way (x itself without z), added as it is; one that reached x = act(z) goes through
+    activation_bwd first.  ws: linear_bwd_workspace()."""
     return _native.linear_bwd(dy, x, w, flags, z, act, residual, want_dx, want_dw, want_dbias, ws)
 
 
