@@ -401,6 +401,8 @@ __device__ __forceinline__ void linear_tile(const LinearStart& p, const LinearAr
     }
     if (apart && !second) barrier_no_fence();
     }
+  } else {
+    wait_vmcnt_le<0>(0);   // (the first stages' loads, which the compiler does not know of: their place is scratch from here on)
   }
   f32x4 sum[S::kFA][S::kOutB];
   add_groups<S>(acc, sum, lds, group, wave, lane);

@@ -159,6 +159,8 @@ __device__ __forceinline__ void product_tile(const ProjStart& p, const ProjArgs&
                                                       [](const bf16x8 (&)[S::kFB]) {}, []() { wait_vmcnt_le<0>(0); }, []() {});
     }
     if (apart && !second) barrier_no_fence();
+  } else {
+    wait_vmcnt_le<0>(0);   // (the first stages' loads, which the compiler does not know of: their place is scratch from here on)
   }
   f32x4 sum[S::kFA][S::kOutB];
   add_groups<S>(acc, sum, lds, group, wave, lane);
