@@ -12,31 +12,12 @@
 #include "activation.h"
 #include "eight_bits.h"
 #include "launch.h"
+#include "row_deal.h"
 
 namespace mate {
 namespace {
 
-constexpr int kThreads = 256, kUnit = 8, kUnits = kScaleBlock / kUnit;   // kUnits: of a scale block
-
-// Which rows a workgroup takes, and the units of a row (those of whole scale blocks).
-struct RowDeal {
-  int rows, E;
-  int each;            // rows of a workgroup
-  unsigned units, by;  // of a row; 2^32 / units, rounded up
-};
-RowDeal deal_rows(int rows, int E) {
-  RowDeal d;
-  d.rows = rows;
-  d.E = E;
-  d.units = (unsigned)kUnits * scale_blocks(E);
-  d.by = (unsigned)(((1ull << 32) + d.units - 1) / d.units);
-  // four units a thread once there are enough for the chip: their loads travel together
-  const size_t total = (size_t)rows * d.units;
-  const unsigned want = total >= (size_t)4 * kThreads * 1024 ? 4 * kThreads : kThreads;
-  d.each = (int)std::max(1u, want / d.units);
-  return d;
-}
-unsigned groups_of(const RowDeal& d) { return (unsigned)((d.rows + (long)d.each - 1) / d.each); }
+constexpr int kThreads = kRowThreads, kUnits = kScaleBlock / kUnit;   // kUnits: of a scale block
 
 // A thread's unit: its row (of the tensor), first feature, and whether there are features there.
 struct Unit {
@@ -44,10 +25,10 @@ struct Unit {
   int first;
   bool some;
 };
-__device__ __forceinline__ Unit unit_at(const RowDeal& d, unsigned i, int here) {
+__device__ __forceinline__ Unit unit_at(const RowDeal& d, long first, unsigned i, int here) {
   const unsigned r = __umulhi(i, d.by);   // (i <= 2^13 and units <= 2^13: the rounding of `by` cannot reach the next quotient)
   Unit u;
-  u.row = (size_t)blockIdx.x * d.each + r;
+  u.row = (size_t)first + r;
   u.first = (int)(i - r * d.units) * kUnit;
   u.some = (int)r < here && u.first < d.E;
   return u;
@@ -95,13 +76,14 @@ __device__ __forceinline__ void values_of(const uint2& w, unsigned s, float (&v)
 // Calls load and then rest for every unit of this workgroup, kDepth of them at a time, all lanes of a wavefront together.
 template <int kDepth, class Load, class Rest>
 __device__ __forceinline__ void each_unit(const RowDeal& d, Load&& load, Rest&& rest) {
-  const int here = (int)min((size_t)d.each, (size_t)d.rows - (size_t)blockIdx.x * d.each);
+  const long first = first_row(d, blockIdx.x, blockIdx.y);
+  const int here = rows_from(d, first);
   const unsigned n = (unsigned)d.each * d.units;
   for (unsigned i0 = threadIdx.x; i0 < n + threadIdx.x; i0 += kDepth * kThreads) {
     Unit u[kDepth];
 #pragma unroll
     for (int k = 0; k < kDepth; ++k) {
-      u[k] = unit_at(d, min(i0 + k * kThreads, n), here);   // (n: past the last row)
+      u[k] = unit_at(d, first, min(i0 + k * kThreads, n), here);   // (n: past the last row)
       load(k, u[k]);
     }
 #pragma unroll
@@ -181,7 +163,7 @@ __global__ __launch_bounds__(kThreads) void activation_bwd_kernel(const void* dy
 template <class Launch>
 hipError_t launch_rows(const RowDeal& d, Launch&& launch) {
   const size_t units = (size_t)d.each * d.units;
-  const dim3 grid(groups_of(d));
+  const dim3 grid = groups_of(d);
   if (units <= kThreads) launch(grid, std::integral_constant<int, 1>());
   else if (units <= 2 * kThreads) launch(grid, std::integral_constant<int, 2>());
   else launch(grid, std::integral_constant<int, 4>());
@@ -192,7 +174,7 @@ hipError_t launch_rows(const RowDeal& d, Launch&& launch) {
 
 hipError_t launch_checkpoint_pack(const void* x, const unsigned char* flags, int rows, int E, bool f32, unsigned char* codes, unsigned char* scales,
                                   hipStream_t stream) {
-  const RowDeal d = deal_rows(rows, E);
+  const RowDeal d = deal_rows(rows, E, kScaleBlock);
   auto run = [&](auto kernel, dim3 grid) { hipLaunchKernelGGL(kernel, grid, dim3(kThreads), 0, stream, x, flags, codes, scales, d); };
   return launch_rows(d, [&](dim3 g, auto depth) {
     constexpr int k = decltype(depth)::value;
@@ -201,7 +183,7 @@ hipError_t launch_checkpoint_pack(const void* x, const unsigned char* flags, int
 }
 
 hipError_t launch_checkpoint_unpack(const unsigned char* codes, const unsigned char* scales, int rows, int E, bool f32, void* x, hipStream_t stream) {
-  const RowDeal d = deal_rows(rows, E);
+  const RowDeal d = deal_rows(rows, E, kScaleBlock);
   auto run = [&](auto kernel, dim3 grid) { hipLaunchKernelGGL(kernel, grid, dim3(kThreads), 0, stream, codes, scales, x, d); };
   return launch_rows(d, [&](dim3 g, auto depth) {
     constexpr int k = decltype(depth)::value;
@@ -211,7 +193,7 @@ hipError_t launch_checkpoint_unpack(const unsigned char* codes, const unsigned c
 
 hipError_t launch_activation_bwd(const void* dy, const void* z, const unsigned char* z_scales, const unsigned char* flags, int rows, int E, int act,
                                  void* dz, hipStream_t stream) {
-  const RowDeal d = deal_rows(rows, E);
+  const RowDeal d = deal_rows(rows, E, kScaleBlock);
   auto run = [&](auto kernel, dim3 grid) { hipLaunchKernelGGL(kernel, grid, dim3(kThreads), 0, stream, dy, z, z_scales, flags, dz, act, d); };
   return launch_rows(d, [&](dim3 g, auto depth) {
     constexpr int k = decltype(depth)::value;
