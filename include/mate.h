@@ -354,7 +354,7 @@ mate_status mate_out_project_bwd(const void* o, const void* w_o, const uint8_t* 
  *
  * 8 bits.  A tensor of [B, N, W] values is `codes` [B, N, W] uint8, e4m3 (1 sign, 4 exponent, 3 mantissa bits, no
  * infinities), and `scales` [B, N, ceil(W / 32)] uint8, one for each 32 features of a token (the last block may be
- * shorter): value = code * 2^(scale - 127).  A scale is the smallest with the block's largest finite magnitude
+ * shorter): value = code * 2^(scale - 127), which fp32 holds exactly, and bf16 but for values below 2^-130 (rounded there).  A scale is the smallest with the block's largest finite magnitude
  * <= 448 * 2^(scale - 127), at least 1: no finite value saturates, each is off by 2^-4 of itself at most, or
  * by 2^-10 of 2^(scale - 127) if that is more.  Rounded to nearest even (from 1.9375 * 2^127 on down,
  * to 1.875 * 2^127).  Infinities and NaN are kept as NaN.  Rows of PAD tokens

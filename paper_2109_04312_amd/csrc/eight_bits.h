@@ -5,7 +5,8 @@
 // keeps all four of its significant bits.  (The usual choice, the exponent of the largest value less 8, is one smaller for
 // largest mantissas above 1.75, which then saturate, off by up to an eighth.)  Values are rounded to nearest even.
 // A power of two makes the rest exact: dividing by it, and code x scale in bf16, which has four spare mantissa
-// bits and the scale's exponents.  Infinities and NaN are stored as NaN and do not enter the scale; a block of zeros
+// bits and the scale's exponents.  (But for scales 1 and 2: below 2^-130 their values have more bits than bf16's denormal numbers, and are rounded to
+// nearest even; fp32 holds all.)  Infinities and NaN are stored as NaN and do not enter the scale; a block of zeros
 // has s = 1.
 #pragma once
 #include <hip/hip_runtime.h>
@@ -69,7 +70,7 @@ __device__ __forceinline__ unsigned to_codes(float a, float b, float c, float d,
   r = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(r, c, d, scale, true);
   return __builtin_bit_cast(unsigned, r);
 }
-// And back: exact.
+// And back: exact in fp32.
 __device__ __forceinline__ f32x4 from_codes(unsigned w, float scale) {
   const f32x2 a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w, scale, false), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w, scale, true);
   return f32x4{a[0], a[1], b[0], b[1]};

@@ -669,7 +669,7 @@ hipError_t launch_few(const FewForm& f, const LinearArgs& a, hipStream_t stream)
 // workgroup owns a tile of dw and a range of the token blocks; the ranges' sums are added in a fixed order (no atomic
 // additions: the result is bit-reproducible), in the launch (kMerge) or after it.  The bias gradient rides along in the workgroups of the first
 // column tile.  Rows of pad tokens are cleared in LDS after a block has landed, and blocks of padding only are skipped.
-// x in 8 bits (kCodes) passes through registers: 16 codes of a token and their scale become bf16, exactly, on the way to LDS.  That takes
+// x in 8 bits (kCodes) passes through registers: 16 codes of a token and their scale become bf16 (exactly, but for values below 2^-130) on the way to LDS.  That takes
 // a stage a third of a microsecond longer, in every tile that reads them; where a copy in bf16, written and read again, takes
 // less, the values are copied into the workspace first.  (us, dw with a copy and so: 16384 tokens, 4096 x 1024 178 and 151, 1024 x 4096 139 and 152,
 // 4072 tokens, 2048 x 768 36 and 59.)

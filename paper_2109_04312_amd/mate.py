@@ -319,7 +319,7 @@ def checkpoint_pack(x, flags=None, out: Checkpoint | None = None) -> Checkpoint:
 
 
 def checkpoint_unpack(checkpoint: Checkpoint, dtype: torch.dtype = torch.bfloat16, out=None) -> torch.Tensor:
-    """The values that a checkpoint stands for, bf16 or float32 (either holds them exactly)."""
+    """The values that a checkpoint stands for, bf16 or float32: exact, but for those below 2^-130 in bf16, which are rounded."""
     if dtype not in (torch.bfloat16, torch.float32):
         raise TypeError(f"unsupported dtype {dtype}")
     return _native.checkpoint_unpack(checkpoint, dtype == torch.float32, out)

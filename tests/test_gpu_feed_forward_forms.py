@@ -1,6 +1,8 @@
 """Every form that sizes choose in the feed-forward half (tests/test_feed_forward_forms.py holds each size to the form named here), with small whole
 numbers: every product and every partial sum is exact in fp32 in any order (below 2^24), so that results are the oracle's bit for bit, and a
 lost, doubled or misplaced term shows at any width and length."""
+import math
+
 import pytest
 import torch
 
@@ -130,3 +132,18 @@ def test_backward(B, N, E, F, form, how):
         for what, got in (("both", both), ("alone", (only_x[0], only_w[1], only_w[2]))):
             for name, u, v in zip(("dx", "dw", "dbias"), got, (dx, dw, db)):
                 assert torch.equal(u, v), f"{name}, {what}"
+
+
+def test_every_code_at_every_scale():
+    """What a checkpoint stands for, at all scales that packing makes: exact in fp32, and in bf16 from scale 3 on; the nearest bf16 below."""
+    mate = mate_module()
+    codes = torch.arange(256, dtype=torch.uint8, device="cuda").repeat(1, 247, 1)
+    scales = torch.arange(1, 248, dtype=torch.uint8, device="cuda")[None, :, None].repeat(1, 1, 8)
+    kept, want = mate.Checkpoint(codes.contiguous(), scales.contiguous()), ff.values(codes, scales)
+    want = torch.where(want.abs() < 2.0 ** 128, want, math.nan)   # (the largest codes of the largest scales, which packing does not make)
+    nan = torch.isnan(want)
+    for dtype in (torch.float32, torch.bfloat16):
+        got = mate.checkpoint_unpack(kept, dtype)
+        assert torch.equal(got[~nan], want.to(dtype)[~nan])       # (below, want has at most four bits: one rounding, fp32 holds it)
+    exact = ~nan & ((scales >= 3).repeat_interleave(32, -1) | (want.abs() >= 2.0 ** -130))
+    assert torch.equal(got.double()[exact], want[exact]) and not torch.equal(got.double()[~nan], want[~nan])
