@@ -34,7 +34,7 @@ def act(name, z):
     if name == "gelu":
         return z * 0.5 * torch.special.erfc(-z / math.sqrt(2))
     if name == "gelu_tanh":
-        return 0.5 * z * (1 + torch.tanh(SCORE * (z + 0.044715 * z ** 3)))
+        return z * torch.sigmoid(2 * SCORE * (z + 0.044715 * z ** 3))     # (1 + tanh u = 2 sigmoid(2 u), which does not cancel below 0)
     if name == "silu":
         return z * torch.sigmoid(z)
     assert name == "tanh"
@@ -50,9 +50,8 @@ def slope(name, z):
     if name == "gelu":
         return 0.5 * torch.special.erfc(-z / math.sqrt(2)) + z * torch.exp(-z * z / 2) / math.sqrt(2 * math.pi)
     if name == "gelu_tanh":
-        t = torch.tanh(SCORE * (z + 0.044715 * z ** 3))
-        bent = 1 / torch.cosh((SCORE * (z + 0.044715 * z ** 3)).clamp(-300, 300)) ** 2
-        return 0.5 * (1 + t) + 0.5 * z * bent * SCORE * (1 + 3 * 0.044715 * z ** 2)
+        u = 2 * SCORE * (z + 0.044715 * z ** 3)
+        return torch.sigmoid(u) + z * torch.sigmoid(u) * torch.sigmoid(-u) * 2 * SCORE * (1 + 3 * 0.044715 * z ** 2)
     if name == "silu":
         p = torch.sigmoid(z)
         return p * (1 + z * torch.sigmoid(-z))
