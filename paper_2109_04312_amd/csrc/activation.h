@@ -7,11 +7,14 @@
 //   tanh       2 p(2 z) - 1, and below 1/16, where that cancels, z - z^3 / 3 + 2 z^5 / 15; derivative 4 p(2 |z|) (1 - p(2 |z|))
 //   gelu       z F(z), F the normal distribution function;  derivative F(z) + z f(z), f its density
 // gelu is max(z, 0) - |z| F(-|z|), and F(-t) = 2^p(t): its logarithm is smooth, so that a polynomial of degree 7 does (fitted here, for the
-// least largest error; relative to F it is below 2^-10 up to t = 9, and |z| F(-|z|) is off by 2.7e-7 at most, rounding included).  Beyond, p goes on
+// least largest error; relative to F it is below 2^-10 up to t = 9, and |z| F(-|z|) is off by 2.8e-7 at most, rounding included; above 0 the
+// result's own rounding to fp32 comes on top).  Beyond, p goes on
 // falling.  The derivative is S(-z) below 0 and 1 - S(z) above, S(t) = F(-t) - t f(t) = e^(-t^2 / 2) m(t), m a polynomial of degree 10 up
-// to t = 6.5, off by 4.4e-7 with rounding; beyond, where S is below 1e-8, m stays what it is there.  One exponential each and no quotient (a
+// to t = 6.5, off by 4.4e-7 below 0 and, where 1 - S is rounded once more, 5e-7 above (at z = -4 that is a 1700th of the slope, at -5 a 250th, which
+// is bf16's own half step; a polynomial of higher degree would take another slot a value); beyond, where S is below 1e-8, m stays what it is there.
+// gelu and its derivative take one exponential each and no quotient (a
 // hardware one takes as long as four additions): 14 and 21 instruction slots a value, where formula 7.1.26 of Abramowitz and Stegun
-// takes 20 and 24.
+// takes 20 and 24.  The others have one exponential and one reciprocal each.
 #pragma once
 #include <hip/hip_runtime.h>
 
@@ -76,7 +79,7 @@ __device__ __forceinline__ float activate(float z) {
   return z;
 }
 
-// (|z| is cut at 64 where a factor is zero by then: infinity times zero would not be.)
+// (|z| is cut at 64 where another factor is below 2^-92 by then: infinity times zero would not be zero.)
 template <int kAct>
 __device__ __forceinline__ float slope(float z) {
   const float zc = __builtin_fminf(__builtin_fmaxf(z, -64.f), 64.f);
