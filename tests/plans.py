@@ -28,13 +28,13 @@ TILES = ("256", "128", "128x2", "64", "64x2")
 
 @functools.lru_cache(None)
 def lib():
-    d = tempfile.mkdtemp()
-    src, so = os.path.join(d, "plan.hip"), os.path.join(d, "plan.so")
-    with open(src, "w") as f:
-        f.write(SOURCE)
-    subprocess.run(["hipcc", "--offload-arch=gfx950", "--cuda-host-only", "-O1", "-std=c++17", "-fPIC", "-shared", "-w", f"-I{CSRC}", src, "-o", so],
-                   check=True, capture_output=True)
-    return C.CDLL(so)
+    with tempfile.TemporaryDirectory() as d:
+        src, so = os.path.join(d, "plan.hip"), os.path.join(d, "plan.so")
+        with open(src, "w") as f:
+            f.write(SOURCE)
+        subprocess.run(["hipcc", "--offload-arch=gfx950", "--cuda-host-only", "-O1", "-std=c++17", "-fPIC", "-shared", "-w", f"-I{CSRC}", src, "-o", so],
+                       check=True, capture_output=True)
+        return C.CDLL(so)   # (stays mapped)
 
 
 def forward(T, E, F, codes):

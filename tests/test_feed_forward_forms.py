@@ -7,17 +7,22 @@ import pytest
 
 from tests import plans
 from tests import test_gpu_feed_forward as general
+from tests import test_gpu_padding_tiles as padding
 from tests.test_gpu_feed_forward_forms import BACKWARD, FORWARD
 
 
 def test_forward_sizes_take_the_named_forms():
     for B, N, E, F, codes, form in FORWARD:
         assert plans.forward(B * N, E, F, codes) == form, (B, N, E, F, codes)
+    for B, N, E, F, form in padding.FORWARD:
+        assert plans.forward(B * N, E, F, True) == form, (B, N, E, F)
 
 
 def test_backward_sizes_take_the_named_forms():
     for B, N, E, F, form, how in BACKWARD:
         assert plans.backward(B * N, E, F) == (form, how), (B, N, E, F)
+    for B, N, E, F, form in padding.BACKWARD:
+        assert plans.backward(B * N, E, F)[0] == form, (B, N, E, F)
 
 
 def sizes():

@@ -1,11 +1,10 @@
 """Tiles of padding only, which skip the products, beside tiles that do not: the tokens of the others have the bits that they have without any padding, in
-every form (the sum of a token goes by the sizes alone), and padding is zeros whatever it held."""
+every form (the sum of a token goes by the sizes alone; tests/test_feed_forward_forms.py holds each size to its form), and padding is zeros whatever it held."""
 import math
 
 import pytest
 import torch
 
-from tests import plans
 from tests.test_gpu_feed_forward import PAD, Inputs
 
 pytestmark = pytest.mark.gpu
@@ -36,13 +35,14 @@ FORWARD = [(6, 256, 2048, 264, "split 2"), (4, 64, 4104, 776, "split 4"), (6, 25
            (6, 768, 328, 136, "tiles 64x2"), (12, 768, 328, 136, "tiles 128x2"), (6, 512, 40, 1160, "tiles 128"), (6, 768, 72, 2696, "tiles 256")]
 BACKWARD = [(6, 64, 40, 136, "one launches, dw 128 ranges 1, dx 128x2"), (6, 64, 40, 4048, "one launches, dw 128 ranges 1, dx 64x2 split 4"),
             (6, 64, 40, 856, "one launches, dw 128 ranges 1, dx 64x2"), (6, 64, 40, 40, "two launches, dw 128 ranges 1, dx 64"),
-            (6, 128, 3360, 40, "two launches, dw 128 ranges 1, dx 128"), (6, 768, 424, 1032, None), (4, 512, 13992, 72, None), (12, 768, 40, 352, None)]
+            (6, 128, 3360, 40, "two launches, dw 128 ranges 1, dx 128"), (6, 768, 424, 1032, "one launches, dw 128 ranges 4, dx 128x2"),
+            (4, 512, 13992, 72, "two launches, dw 128 ranges 2, dx 128"), (12, 768, 40, 352, "two launches, dw 128 ranges 9, dx 64x2")]
 
 
 @pytest.mark.parametrize("B,N,E,F,form", FORWARD)
 def test_linear(B, N, E, F, form):
     mate = mate_module()
-    assert plans.forward(B * N, E, F, True) == form
+    print(form, flush=True)
     i = Inputs(N, B, N, E, F, None)
     flags = some_sequences_only(B, N)
     kw = dict(act=mate.MATE_ACT_GELU, keep_z=mate.MATE_KEEP_8BIT, keep_y=True)
@@ -59,7 +59,7 @@ def test_linear(B, N, E, F, form):
 @pytest.mark.parametrize("B,N,E,F,form", BACKWARD)
 def test_linear_bwd(B, N, E, F, form):
     mate = mate_module()
-    assert form is None or plans.backward(B * N, E, F)[0] == form
+    print(form, flush=True)
     i = Inputs(N, B, N, E, F, None)
     flags = some_sequences_only(B, N)
     zeroed = torch.where((flags == PAD)[..., None], 0, i.dy)
