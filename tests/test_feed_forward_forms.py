@@ -1,5 +1,5 @@
 """Which form of the feed-forward half a size takes (csrc/linear_plan.h, compiled for the host): the GPU tests' sizes take the forms that they name, and
-no form that any size takes is without one.  A change of the costs that the choice goes by shows here."""
+no form that one of 40000 drawn sizes takes is without a test.  A change of the costs that the choice goes by shows here."""
 import math
 import random
 
